@@ -215,7 +215,8 @@ int sidp_decode_step(sidp_handle *h, float *hidden, const int32_t *positions, co
                      int32_t max_blocks_per_seq, int32_t batch, int32_t flags, void *compute, void *copy);
 /* Waits for all work the handle enqueued on both streams; returns
  * SIDP_EINVAL if a kernel latched a device-side input error since the last
- * sync (and clears it), SIDP_EHIP on an asynchronous HIP error. */
+ * sync (and clears it), SIDP_ENOBLOCKS if sidp_kv_extend ran out of blocks and
+ * nothing else was latched, SIDP_EHIP on an asynchronous HIP error. */
 int sidp_sync(sidp_handle *h);
 
 /* ---- timing ----
@@ -473,6 +474,125 @@ int sidp_rope_append(sidp_handle *h, const void *qkv, const int32_t *positions, 
 int sidp_attention(sidp_handle *h, const void *q, int32_t region, const int32_t *positions,
                    const int32_t *block_tables, int32_t max_blocks_per_seq, int32_t batch, void *out,
                    void *stream);
+/* ---- several new tokens a sequence ----
+ * The calls around a decode step that take any number of new tokens of each
+ * sequence at once: prompts, chunks of prompts, drafted tokens, or one each.
+ * The new tokens of a call are its rows, sequence after sequence: sequence b's
+ * are rows row_starts[b] .. row_starts[b + 1] - 1. They take no scratch of the
+ * handle: unlike the calls above they are not ordered with other calls on the
+ * handle (on one stream they run in order, across streams the caller orders
+ * them), and they may be captured into a graph. Each runs on the handle's
+ * device, whichever is current. Arrays that a call writes may not overlap others
+ * of the same call. Rows behind the last one in use are left as they were. */
+#define SIDP_MAX_ROWS (1 << 20) /* most rows of one call */
+
+/* Block tables, row starts, positions and cache slots of one iteration, made on
+ * the GPU from request lengths (sidp_kv_alloc's tables are made on the host).
+ *  ctx_lens     device int32 [batch]: tokens already cached per sequence.
+ *  new_lens     device int32 [batch]: new tokens this iteration, 0 for none.
+ *  free_blocks  device int32 [num_free]: physical blocks to hand out, in order.
+ *  taken        device int32 [1]: how many of free_blocks are handed out already.
+ *  taken_out    device int32 [1]: receives taken plus the blocks handed out here
+ *               (may be taken itself; that costs a second small launch).
+ *  block_tables device int32 [batch, max_blocks_per_seq]: row b holds the blocks
+ *               of the ctx_lens[b] cached tokens; the entries of new blocks are
+ *               added, the others are left as they were.
+ *  row_starts   device int32 [batch + 1], positions and slots device int32
+ *               [max_rows]: receive the rows; a row's slot is block * 16 + offset.
+ * Sequence b needs ceil((ctx + new) / 16) - ceil(ctx / 16) blocks more; they are
+ * dealt in batch order. The first sequence whose blocks or rows do not fit into
+ * free_blocks or max_rows, and every one behind it, gets no rows and no blocks
+ * (row_starts tells), and sidp_sync returns SIDP_ENOBLOCKS (blocks) or
+ * SIDP_EINVAL (rows). A sequence with a negative length or more tokens than its
+ * table holds gets none and latches SIDP_EINVAL; the others are served. A block
+ * outside the attached cache gives the slot -1 and latches SIDP_EINVAL.
+ * batch 1..SIDP_EXTEND_MAX_BATCH, max_blocks_per_seq at most 65536. */
+#define SIDP_EXTEND_MAX_BATCH 4096
+int sidp_kv_extend(sidp_handle *h, const int32_t *ctx_lens, const int32_t *new_lens, int32_t batch,
+                   const int32_t *free_blocks, int32_t num_free, const int32_t *taken, int32_t *taken_out,
+                   int32_t *block_tables, int32_t max_blocks_per_seq, int32_t max_rows, int32_t *row_starts,
+                   int32_t *positions, int32_t *slots, void *stream);
+
+/* Rotary positions other than the config's (all pairs (i, i + D/2), unscaled). */
+#define SIDP_ROPE_HALF        0 /* pairs (i, i + rotary_dim / 2) */
+#define SIDP_ROPE_INTERLEAVED 1 /* pairs (2 i, 2 i + 1)          */
+#define SIDP_ROPE_SCALE_NONE   0
+#define SIDP_ROPE_SCALE_LINEAR 1 /* every frequency divided by factor */
+#define SIDP_ROPE_SCALE_LLAMA3 2 /* frequencies scaled in bands (Llama 3.1) */
+#define SIDP_ROPE_SCALE_YARN   3 /* YaRN, arXiv 2309.00071 */
+typedef struct sidp_rope {
+  int32_t layout;       /* SIDP_ROPE_HALF or SIDP_ROPE_INTERLEAVED                             */
+  int32_t rotary_dim;   /* leading dims of each head that are turned: 16..D, a multiple of 16  */
+  int32_t scaling;      /* SIDP_ROPE_SCALE_*                                                   */
+  int32_t original_len; /* LLAMA3, YARN: context length that the model was first trained on    */
+  float theta;          /* base, > 1                                                           */
+  float factor;         /* LINEAR, LLAMA3, YARN: how many times longer the contexts are, > 0   */
+  float low_freq, high_freq;   /* LLAMA3: turns in original_len below which a frequency is divided
+                                * by factor, and above which it is kept (usually 1 and 4)      */
+  float beta_slow, beta_fast;  /* YARN: the same for the ends of its ramp (usually 1 and 32)   */
+  float attn_factor;    /* YARN: scale of cos and sin; 0: 0.1 ln(factor) + 1 (factor >= 1)     */
+} sidp_rope;
+/* The angle per position of each of the rotary_dim / 2 pairs (freqs) and the
+ * factor on cos and sin (host only). With w = theta^(-2 i / rotary_dim): LINEAR
+ * w / factor; LLAMA3 keep * w + (1 - keep) * w / factor with keep = (turns -
+ * low_freq) / (high_freq - low_freq) held to 0..1 and turns = original_len * w /
+ * (2 pi); YARN the same blend with keep falling from 1 to 0 along the pair index i
+ * from floor(i(beta_fast)) to ceil(i(beta_slow)), i(n) = rotary_dim ln(original_len
+ * / (2 pi n)) / (2 ln theta). SIDP_EINVAL for values outside those above. */
+int sidp_rope_frequencies(const sidp_rope *rope, int32_t head_dim, double *freqs, double *scale);
+/* Makes `rope` the rotary positions of the handle, for decode steps as for the
+ * single calls (NULL: the config's again). Waits for the device, then writes the
+ * tables (double precision on the host, stored as fp32): a set-up call, not one
+ * for the time between steps; no other call on the handle may overlap it, nor may
+ * it be called under capture. Keys cached before keep the positions they were
+ * stored with. SIDP_EINVAL as sidp_rope_frequencies. */
+int sidp_set_rope(sidp_handle *h, const sidp_rope *rope);
+
+/* QK-norm (when configured), RoPE and KV append of many rows at given positions
+ * and slots: sidp_rope_append for several tokens a sequence.
+ *  qkv        device bf16 [rows, qkv_stride], the first (Hq + 2 Hkv) D of each row
+ *             used; 16-byte aligned, qkv_stride a multiple of 8.
+ *  row_count  device int32 [1]: rows in use, at most `rows` (row_starts[batch] of
+ *             sidp_kv_extend, say); NULL: all.
+ *  positions  device int32 [rows]; one outside [0, max_seq_len) latches SIDP_EINVAL
+ *             and its row is left out.
+ *  slots      device int32 [rows]: block * 16 + offset in region `region`; a
+ *             negative one caches nothing (the query is still written), one past
+ *             the region latches SIDP_EINVAL as well. Two rows may not share one.
+ *  g_q, g_k   device bf16 [D], 16-byte aligned; read when the config has QK-norm.
+ *  q_out      device bf16 [rows, Hq, D], 16-byte aligned. */
+int sidp_rope_append_rows(sidp_handle *h, const void *qkv, int64_t qkv_stride, int32_t rows, const int32_t *row_count,
+                          const int32_t *positions, const int32_t *slots, const void *g_q, const void *g_k,
+                          int32_t region, void *q_out, void *stream);
+
+/* ---- answers ----
+ * Log probabilities of given tokens, their ranks, the entropy and the most likely
+ * tokens of each row of logits (the output projection of sidp_linear, say), on the
+ * current device.
+ *  logits       device [rows, row_stride], the first `vocab` of each row used;
+ *               bf16 or fp32 by `dtype`, aligned to its type.
+ *  targets      device int32 [rows]: the given tokens; one outside [0, vocab) is
+ *               none (log probability NaN, rank -1). NULL: none at all.
+ *  logprobs     device fp32 [rows] or NULL: x_target - log sum exp x.
+ *  ranks        device int32 [rows] or NULL: logits above the target's.
+ *  entropies    device fp32 [rows] or NULL: -sum p log p, in nats.
+ *  top_ids, top_logprobs  device [rows, top_k]: the top_k most likely tokens, of
+ *               equal logits the lowest token first.
+ * -inf is a masked token (probability 0). A row without a distribution (a NaN or
+ * +inf, or nothing but -inf) gets NaN, rank -1 and ids -1.
+ *  workspace    device, 16-byte aligned, sidp_token_logprobs_bytes of the same
+ *               sizes; nothing in it outlives the call, but calls that overlap in
+ *               time may not share one. */
+#define SIDP_LOGITS_BF16 0
+#define SIDP_LOGITS_F32  1
+#define SIDP_LOGPROBS_MAX_TOP   32
+#define SIDP_LOGPROBS_MAX_VOCAB (1 << 20)
+/* 0 for sizes that sidp_token_logprobs refuses. */
+size_t sidp_token_logprobs_bytes(int32_t rows, int32_t vocab, int32_t top_k);
+int sidp_token_logprobs(const void *logits, int32_t dtype, int32_t rows, int32_t vocab, int64_t row_stride,
+                        const int32_t *targets, int32_t top_k, float *logprobs, int32_t *ranks, float *entropies,
+                        int32_t *top_ids, float *top_logprobs, void *workspace, size_t workspace_bytes, void *stream);
+
 /* Device-to-device copy by the library's copy kernel (the slot-fill engine),
  * using `grid` workgroups (0 = default). src, dst 16-byte aligned. */
 int sidp_copy(const void *src, void *dst, size_t bytes, int32_t grid, void *stream);

@@ -54,10 +54,21 @@ EXPORTED = [
     "sidp_pack_gate_up", "sidp_linear", "sidp_slot_mapping", "sidp_rope_append", "sidp_attention", "sidp_copy",
     "sidp_timing_collect", "sidp_set_pooling", "sidp_cas_ffn", "sidp_timing_select", "sidp_mode_update",
     "sidp_set_fill_tiles", "sidp_debug_inject_hip_error", "sidp_linear_noalloc", "sidp_linear_plan",
-    "sidp_attention_plan",
+    "sidp_attention_plan", "sidp_kv_extend", "sidp_rope_frequencies", "sidp_set_rope", "sidp_rope_append_rows",
+    "sidp_token_logprobs_bytes", "sidp_token_logprobs",
 ]
 
 SIDP_CAS_MAX_REPLICAS = 16
+
+SIDP_ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+SIDP_ROPE_SCALINGS = {"none": 0, "linear": 1, "llama3": 2, "yarn": 3}
+
+SIDP_LOGITS_BF16 = 0
+SIDP_LOGITS_F32 = 1
+SIDP_LOGPROBS_MAX_TOP = 32
+SIDP_LOGPROBS_MAX_VOCAB = 1 << 20
+SIDP_EXTEND_MAX_BATCH = 4096
+SIDP_MAX_ROWS = 1 << 20
 
 
 class SidpError(RuntimeError):
@@ -71,6 +82,12 @@ class sidp_config(ctypes.Structure):
         "num_layers", "hidden", "num_q_heads", "num_kv_heads", "head_dim", "ffn_dim", "qkv_bias", "qk_norm",
         "block_size", "max_batch", "max_seq_len")] + [
         ("rms_eps", ctypes.c_float), ("qk_norm_eps", ctypes.c_float), ("rope_theta", ctypes.c_float)]
+
+
+class sidp_rope(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("layout", "rotary_dim", "scaling", "original_len")] + [
+        (n, ctypes.c_float) for n in (
+            "theta", "factor", "low_freq", "high_freq", "beta_slow", "beta_fast", "attn_factor")]
 
 
 class sidp_mode_policy(ctypes.Structure):
@@ -104,6 +121,7 @@ _P = ctypes.c_void_p
 _I = ctypes.c_int32
 _Z = ctypes.c_size_t
 _PI = ctypes.POINTER(ctypes.c_int32)
+_PD = ctypes.POINTER(ctypes.c_double)
 _sigs = {
     "sidp_strerror": (ctypes.c_char_p, [ctypes.c_int]),
     "sidp_last_hip_error": (ctypes.c_int, [_P]),
@@ -138,6 +156,12 @@ _sigs = {
     "sidp_slot_mapping": (ctypes.c_int, [_P, _P, _P, _I, _I, _P, _P]),
     "sidp_rope_append": (ctypes.c_int, [_P, _P, _P, _P, _I, _I, _P, _P, _I, _P, _P]),
     "sidp_attention": (ctypes.c_int, [_P, _P, _I, _P, _P, _I, _I, _P, _P]),
+    "sidp_kv_extend": (ctypes.c_int, [_P, _P, _P, _I, _P, _I, _P, _P, _P, _I, _I, _P, _P, _P, _P]),
+    "sidp_rope_frequencies": (ctypes.c_int, [ctypes.POINTER(sidp_rope), _I, _PD, _PD]),
+    "sidp_set_rope": (ctypes.c_int, [_P, ctypes.POINTER(sidp_rope)]),
+    "sidp_rope_append_rows": (ctypes.c_int, [_P, _P, ctypes.c_int64, _I, _P, _P, _P, _P, _P, _I, _P, _P]),
+    "sidp_token_logprobs_bytes": (_Z, [_I, _I, _I]),
+    "sidp_token_logprobs": (ctypes.c_int, [_P, _I, _I, _I, ctypes.c_int64, _P, _I, _P, _P, _P, _P, _P, _P, _Z, _P]),
     "sidp_copy": (ctypes.c_int, [_P, _P, _Z, _I, _P]),
     "sidp_timing_collect": (ctypes.c_int, [_P, ctypes.POINTER(ctypes.c_double), _PI]),
     "sidp_mode_update": (ctypes.c_int, [ctypes.POINTER(sidp_mode_policy), ctypes.POINTER(sidp_mode_state), _I, _PI,
@@ -390,6 +414,51 @@ def sidp_rope_append(h, qkv, positions, block_tables, max_blocks_per_seq, batch,
 def sidp_attention(h, q, region, positions, block_tables, max_blocks_per_seq, batch, out, stream=None):
     _check(_lib.sidp_attention(h, _ptr(q), region, _ptr(positions), _ptr(block_tables), max_blocks_per_seq, batch,
                                _ptr(out), _stream(stream)), "sidp_attention")
+
+
+def sidp_kv_extend(h, ctx_lens, new_lens, batch, free_blocks, num_free, taken, taken_out, block_tables,
+                   max_blocks_per_seq, max_rows, row_starts, positions, slots, stream=None):
+    _check(_lib.sidp_kv_extend(h, _ptr(ctx_lens), _ptr(new_lens), batch, _ptr(free_blocks), num_free, _ptr(taken),
+                               _ptr(taken_out), _ptr(block_tables), max_blocks_per_seq, max_rows, _ptr(row_starts),
+                               _ptr(positions), _ptr(slots), _stream(stream)), "sidp_kv_extend")
+
+
+def make_rope(layout="half", rotary_dim=128, theta=10000.0, scaling="none", factor=1.0, original_len=0, low_freq=1.0,
+              high_freq=4.0, beta_slow=1.0, beta_fast=32.0, attn_factor=0.0):
+    """sidp_rope from names (layout: SIDP_ROPE_LAYOUTS, scaling: SIDP_ROPE_SCALINGS) and numbers."""
+    return sidp_rope(SIDP_ROPE_LAYOUTS[layout], rotary_dim, SIDP_ROPE_SCALINGS[scaling], original_len, theta, factor,
+                     low_freq, high_freq, beta_slow, beta_fast, attn_factor)
+
+
+def sidp_rope_frequencies(rope, head_dim):
+    """(angle per position of each pair, factor on cos and sin), host only."""
+    freqs = (ctypes.c_double * 64)()
+    scale = ctypes.c_double()
+    _check(_lib.sidp_rope_frequencies(ctypes.byref(rope), head_dim, freqs, ctypes.byref(scale)),
+           "sidp_rope_frequencies")
+    return list(freqs[:rope.rotary_dim // 2]), scale.value
+
+
+def sidp_set_rope(h, rope):
+    """rope: from make_rope, or None for the config's own."""
+    _check(_lib.sidp_set_rope(h, None if rope is None else ctypes.byref(rope)), "sidp_set_rope")
+
+
+def sidp_rope_append_rows(h, qkv, qkv_stride, rows, row_count, positions, slots, g_q, g_k, region, q_out, stream=None):
+    _check(_lib.sidp_rope_append_rows(h, _ptr(qkv), qkv_stride, rows, _ptr(row_count), _ptr(positions), _ptr(slots),
+                                      _ptr(g_q), _ptr(g_k), region, _ptr(q_out), _stream(stream)),
+           "sidp_rope_append_rows")
+
+
+def sidp_token_logprobs_bytes(rows, vocab, top_k):
+    return _lib.sidp_token_logprobs_bytes(rows, vocab, top_k)
+
+
+def sidp_token_logprobs(logits, dtype, rows, vocab, row_stride, targets, top_k, logprobs, ranks, entropies, top_ids,
+                        top_logprobs, workspace, workspace_bytes, stream=None):
+    _check(_lib.sidp_token_logprobs(_ptr(logits), dtype, rows, vocab, row_stride, _ptr(targets), top_k, _ptr(logprobs),
+                                    _ptr(ranks), _ptr(entropies), _ptr(top_ids), _ptr(top_logprobs), _ptr(workspace),
+                                    workspace_bytes, _stream(stream)), "sidp_token_logprobs")
 
 
 def sidp_copy(src, dst, nbytes, grid=0, stream=None):

@@ -12,6 +12,7 @@ typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
 // Device-side input error bits, latched in the handle's error word.
 #define SIDP_DEVERR_POSITION 0x1u  // position outside the block table
 #define SIDP_DEVERR_BLOCK    0x2u  // block index outside the KV region
+#define SIDP_DEVERR_NOBLOCKS 0x4u  // free list exhausted
 
 __device__ __forceinline__ float bf2f(uint16_t b) { return __uint_as_float(((uint32_t)b) << 16); }
 

@@ -4,6 +4,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <algorithm>
+
 #include "../../include/sidp.h"
 
 namespace sidp {
@@ -79,6 +81,8 @@ struct RopeCall {
   const float* rope_cos;  // [max_seq][D/2]
   const float* rope_sin;
   int max_seq;
+  int rot;                // leading dims that are turned, a multiple of 16
+  bool interleaved;       // pairs (2 i, 2 i + 1) instead of (i, i + rot / 2)
   KvView kv;
   int region;
   uint16_t* q_out;
@@ -88,6 +92,79 @@ struct RopeCall {
 hipError_t launch_rope_append(const RopeCall& c, hipStream_t s);
 hipError_t launch_slot_mapping(const int32_t* positions, const int32_t* bt, int max_blocks, int batch, int bs,
                                int nblk, int32_t* slots, uint32_t* err, hipStream_t s);
+
+// Many rows at given positions and cache slots: see sidp_rope_append_rows.
+struct RopeRowsCall {
+  const uint16_t* qkv;       // [rows][stride]
+  int64_t stride;
+  int rows;
+  const int32_t* row_count;  // rows in use, or null
+  const int32_t* positions;
+  const int32_t* slots;
+  int hq, hkv;
+  const uint16_t* g_q;
+  const uint16_t* g_k;
+  float qk_eps;
+  const float* rope_cos;
+  const float* rope_sin;
+  int max_seq, rot;
+  bool interleaved;
+  KvView kv;
+  int region;
+  uint16_t* q_out;
+  uint32_t* err;
+  int num_cus;
+};
+hipError_t launch_rope_rows(const RopeRowsCall& c, hipStream_t s);
+
+// Angle per position of the rot / 2 pairs, in turning order, and the factor on
+// cos and sin (host only). False for a rope that a head of `head_dim` cannot have.
+bool rope_frequencies(const sidp_rope& r, int head_dim, double* freqs, double* scale);
+// cos and sin tables [positions][head_dim / 2] (host): entry p, i is the cosine of
+// p * freqs[i] in double precision, times scale, stored as fp32; 0 from `pairs` on.
+void rope_tables(const double* freqs, int pairs, double scale, int positions, int head_dim, float* cos, float* sin);
+
+constexpr int kBlockTokens = 16;  // tokens of a KV block
+
+struct ExtendCall {
+  const int32_t* ctx_lens;
+  const int32_t* new_lens;
+  int batch;
+  const int32_t* free_blocks;
+  int num_free;
+  const int32_t* taken;
+  int32_t* taken_out;
+  int32_t* block_tables;
+  int max_blocks;
+  int max_rows;
+  int nblk;
+  int32_t* row_starts;
+  int32_t* positions;
+  int32_t* slots;
+  uint32_t* err;
+};
+hipError_t launch_kv_extend(ExtendCall c, hipStream_t s);
+
+struct LogprobCall {
+  const void* logits;
+  bool f32;
+  int rows, vocab;
+  int64_t stride;
+  const int32_t* targets;
+  int top;
+  float* logprob;
+  int32_t* rank;
+  float* entropy;
+  int32_t* top_ids;
+  float* top_logprobs;
+  void* ws;
+  // set by launch_logprobs
+  int slices = 0;
+  void* stats = nullptr;
+  void* keys = nullptr;
+};
+size_t logprob_ws_bytes(int rows, int vocab, int top);
+hipError_t launch_logprobs(LogprobCall c, hipStream_t s);
 
 struct AttnCall {
   const uint16_t* q;  // [B][Hq][D]

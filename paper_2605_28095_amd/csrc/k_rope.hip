@@ -12,51 +12,12 @@
 // same value the projection's own reduction would have stored.
 #include "common.h"
 #include "internal.h"
+#include "rope.h"
 
 namespace sidp {
 
-// 8 bf16 values; ALIGNED: 16-byte aligned, one load.
-template <bool ALIGNED>
-__device__ __forceinline__ void load8(const uint16_t* p, float (&v)[8]) {
-  if (ALIGNED) {
-    const u32x4_t u = *(const u32x4_t*)p;
-#pragma unroll
-    for (int i = 0; i < 4; i++) {
-      v[2 * i] = bf2f((uint16_t)(u[i] & 0xffffu));
-      v[2 * i + 1] = bf2f((uint16_t)(u[i] >> 16));
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; i++) v[i] = bf2f(p[i]);
-  }
-}
-
-// The sum of a head's squares, on each of its D / 8 lanes: rotate-half pairs (i, i +
-// D/2) first, then pairs of i that differ in their highest bit, and so on down, so
-// that the roundings are those of one pair per lane and a butterfly over the lanes.
-// Each of the first steps hands half of a lane's sums over and keeps the other half.
-template <int D>
-__device__ __forceinline__ float head_sum_sq(const float (&x)[8], int sub) {
-  constexpr int kLanes = D / 8;
-  const bool h4 = sub & (kLanes / 2), h2 = sub & (kLanes / 4), h1 = sub & (kLanes / 8);
-  float t[4], u[2];
-#pragma unroll
-  for (int j = 0; j < 4; j++) {  // dims j of the lane's eight in its first half, 4 + j in its second
-    const float own = h4 ? x[4 + j] : x[j];
-    const float other = __shfl_xor(h4 ? x[j] : x[4 + j], kLanes / 2, 64);
-    const float lo = h4 ? other : own, hi = h4 ? own : other;
-    t[j] = fmaf(hi, hi, lo * lo);
-  }
-#pragma unroll
-  for (int j = 0; j < 2; j++) u[j] = (h2 ? t[2 + j] : t[j]) + __shfl_xor(h2 ? t[j] : t[2 + j], kLanes / 4, 64);
-  float v = (h1 ? u[1] : u[0]) + __shfl_xor(h1 ? u[0] : u[1], kLanes / 8, 64);
-  if (D == 128) v += __shfl_xor(v, 1, 64);
-#pragma unroll
-  for (int o = kLanes / 2; o >= kLanes / 8; o >>= 1) v += __shfl_xor(v, o, 64);
-  return v;
-}
-
-template <int D, bool ALIGNED>
+// GENERAL: pairs (2 i, 2 i + 1), or fewer turned dims than the head has.
+template <int D, bool ALIGNED, bool GENERAL>
 __global__ void __launch_bounds__(256) k_rope_append(RopeCall c) {
   constexpr int kLanes = D / 8;         // lanes of a head
   constexpr int kHeads = 256 / kLanes;  // heads of a workgroup
@@ -133,24 +94,30 @@ __global__ void __launch_bounds__(256) k_rope_append(RopeCall c) {
 #pragma unroll
     for (int i = 0; i < 8; i++) x[i] = x[i] * r * g[i];
   }
-  const int t0 = d0 % (D / 2);  // the pair's angle index
-  const float* cs = c.rope_cos + (int64_t)rpos * (D / 2) + t0;
-  const float* sn = c.rope_sin + (int64_t)rpos * (D / 2) + t0;
-  const float sign = d0 < D / 2 ? -1.f : 1.f;
-  uint32_t y[4];
+  u32x4_t out;
+  if (GENERAL) {
+    Turn t;
+    load_turn(c.rope_cos + (int64_t)rpos * (D / 2), c.rope_sin + (int64_t)rpos * (D / 2), c.rot, c.interleaved,
+              threadIdx.x & 63, sub, t);
+    out = c.interleaved ? turned<true>(x, t) : turned<false>(x, t);
+  } else {
+    const int t0 = d0 % (D / 2);  // the pair's angle index
+    const float* cs = c.rope_cos + (int64_t)rpos * (D / 2) + t0;
+    const float* sn = c.rope_sin + (int64_t)rpos * (D / 2) + t0;
+    const float sign = d0 < D / 2 ? -1.f : 1.f;
 #pragma unroll
-  for (int i = 0; i < 8; i += 4) {
-    const f32x4_t cv = *(const f32x4_t*)(cs + i), sv = *(const f32x4_t*)(sn + i) * sign;
-    float o[4];
+    for (int i = 0; i < 8; i += 4) {
+      const f32x4_t cv = *(const f32x4_t*)(cs + i), sv = *(const f32x4_t*)(sn + i) * sign;
+      float o[4];
 #pragma unroll
-    for (int j = 0; j < 4; j++) {
-      const float other = __shfl_xor(x[i + j], kLanes / 2, 64);
-      o[j] = fmaf(x[i + j], cv[j], other * sv[j]);
+      for (int j = 0; j < 4; j++) {
+        const float other = __shfl_xor(x[i + j], kLanes / 2, 64);
+        o[j] = fmaf(x[i + j], cv[j], other * sv[j]);
+      }
+      out[i / 2] = pack_bf2(o[0], o[1]);
+      out[i / 2 + 1] = pack_bf2(o[2], o[3]);
     }
-    y[i / 2] = pack_bf2(o[0], o[1]);
-    y[i / 2 + 1] = pack_bf2(o[2], o[3]);
   }
-  const u32x4_t out = {y[0], y[1], y[2], y[3]};
   if (is_q) {
     uint16_t* qo = c.q_out + ((int64_t)b * c.hq + h) * D + d0;
     if (ALIGNED) {
@@ -273,14 +240,15 @@ static hipError_t launch_rope_d(const RopeCall& c, hipStream_t s) {
   const int per = 256 / (D / 8), heads = c.hq + 2 * c.hkv;
   const dim3 grid(c.batch, (heads + per - 1) / per);
   const uintptr_t ptrs = (uintptr_t)c.qkv | (uintptr_t)c.bias | (uintptr_t)c.g_q | (uintptr_t)c.g_k | (uintptr_t)c.q_out;
-  if (ptrs % 16 == 0) k_rope_append<D, true><<<grid, 256, 0, s>>>(c);
-  else k_rope_append<D, false><<<grid, 256, 0, s>>>(c);
+  const bool general = c.interleaved || c.rot != D;
+  if (ptrs % 16 == 0) general ? k_rope_append<D, true, true><<<grid, 256, 0, s>>>(c) : k_rope_append<D, true, false><<<grid, 256, 0, s>>>(c);
+  else general ? k_rope_append<D, false, true><<<grid, 256, 0, s>>>(c) : k_rope_append<D, false, false><<<grid, 256, 0, s>>>(c);
   return hipGetLastError();
 }
 
 hipError_t launch_rope_append(const RopeCall& c, hipStream_t s) {
   if (c.batch <= 0) return hipSuccess;
-  if (c.beside_fill) {
+  if (c.beside_fill && !c.interleaved && c.rot == c.d) {
     k_rope_append_wave<<<dim3(c.batch, (c.hq + 2 * c.hkv + 3) / 4), 256, 0, s>>>(c);
     return hipGetLastError();
   }

@@ -21,6 +21,7 @@
 #include <vector>
 
 #include "../../include/sidp.h"
+#include "common.h"
 #include "internal.h"
 
 using namespace sidp;
@@ -34,6 +35,7 @@ constexpr int kFillPartAPercent = 25;  // share of a layer's fill issued before 
 constexpr int kFillSmallBatch = 160;   // below this many rows both fill tiles keep 8 loads per lane in flight
 constexpr int kFillLongBatch = 384;    // from this many rows the projections outlast a gentle tile B
 constexpr int kTableUnit = 2048;  // block tables may be as wide as max_seq_len rounded up to this many tokens
+constexpr int kMaxPairs = 64;          // rotary pairs of a head of 128 dims
 constexpr int kBurstGrid = 512;        // workgroups of the whole-chip burst copy (SIDP_COPY_BURST)
 
 size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
@@ -188,6 +190,8 @@ struct sidp_handle {
   uint16_t* g_attn_all = nullptr;
   float* cas_y = nullptr;  // owner-side FFN output of the concatenated CaS rows [max_batch][H] fp32
   float *rope_cos = nullptr, *rope_sin = nullptr;
+  int rope_rot = 0;               // leading dims of a head that are turned
+  bool rope_interleaved = false;  // pairs (2 i, 2 i + 1) instead of (i, i + rope_rot / 2)
   uint32_t* err = nullptr;
   hipEvent_t filled[kSlots] = {}, consumed[kSlots] = {}, mid[kSlots] = {};
   // A slot's fill is two launches on the copy stream, tiles A and B;
@@ -298,6 +302,33 @@ static void free_device(sidp_handle* h) {
   for (hipEvent_t e : h->event_pool) (void)hipEventDestroy(e);
 }
 
+// Puts the cos and sin tables of `pairs` frequencies into the handle's tables.
+static int load_rope(sidp_handle* h, const double* freqs, int pairs, double scale) {
+  const int D = h->cfg.head_dim;
+  const size_t n = (size_t)h->cfg.max_seq_len * (D / 2);
+  std::vector<float> cs, sn;
+  try {
+    cs.resize(n);
+    sn.resize(n);
+  } catch (const std::bad_alloc&) {
+    return SIDP_ENOMEM;
+  }
+  rope_tables(freqs, pairs, scale, h->cfg.max_seq_len, D, cs.data(), sn.data());
+  HIPCHK(h, hipMemcpy(h->rope_cos, cs.data(), n * 4, hipMemcpyHostToDevice));
+  HIPCHK(h, hipMemcpy(h->rope_sin, sn.data(), n * 4, hipMemcpyHostToDevice));
+  return SIDP_OK;
+}
+
+// The config's own rope: every pair (i, i + D/2), angle p * theta^(-2i/D).
+static int load_default_rope(sidp_handle* h) {
+  const int D = h->cfg.head_dim;
+  double freqs[kMaxPairs];
+  for (int i = 0; i < D / 2; i++) freqs[i] = std::pow((double)h->cfg.rope_theta, -2.0 * (double)i / (double)D);
+  h->rope_rot = D;
+  h->rope_interleaved = false;
+  return load_rope(h, freqs, D / 2, 1.0);
+}
+
 int sidp_create(const sidp_config* cfg, sidp_handle** out) {
   if (!out) return SIDP_EINVAL;
   *out = nullptr;
@@ -353,16 +384,8 @@ int sidp_create(const sidp_config* cfg, sidp_handle** out) {
     if (hipMalloc(a.p, a.bytes) != hipSuccess) return fail(SIDP_ENOMEM);
   if (hipMemset(h->err, 0, 256) != hipSuccess) return fail(SIDP_EHIP);
 
-  // RoPE table: angle p * theta^(-2i/D) in double, stored as fp32 cos/sin.
-  std::vector<float> cs((size_t)c.max_seq_len * (D / 2)), sn(cs.size());
-  for (int p = 0; p < c.max_seq_len; p++)
-    for (size_t i = 0; i < D / 2; i++) {
-      const double ang = (double)p * std::pow((double)c.rope_theta, -2.0 * (double)i / (double)D);
-      cs[(size_t)p * (D / 2) + i] = (float)std::cos(ang);
-      sn[(size_t)p * (D / 2) + i] = (float)std::sin(ang);
-    }
-  if (hipMemcpy(h->rope_cos, cs.data(), cs.size() * 4, hipMemcpyHostToDevice) != hipSuccess) return fail(SIDP_EHIP);
-  if (hipMemcpy(h->rope_sin, sn.data(), sn.size() * 4, hipMemcpyHostToDevice) != hipSuccess) return fail(SIDP_EHIP);
+  const int rope = load_default_rope(h);
+  if (rope != SIDP_OK) return fail(rope);
   for (int i = 0; i < kSlots; i++) {
     if (hipEventCreateWithFlags(&h->filled[i], hipEventDisableTiming) != hipSuccess) return fail(SIDP_EHIP);
     if (hipEventCreateWithFlags(&h->tile_a[i], hipEventDisableTiming) != hipSuccess) return fail(SIDP_EHIP);
@@ -618,6 +641,8 @@ static hipError_t run_attn_half(sidp_handle* h, const uint8_t* wb, int layer, fl
   r.rope_cos = h->rope_cos;
   r.rope_sin = h->rope_sin;
   r.max_seq = c.max_seq_len;
+  r.rot = h->rope_rot;
+  r.interleaved = h->rope_interleaved;
   r.kv = kv_view(h);
   r.region = layer % h->regions;
   r.q_out = h->q;
@@ -968,7 +993,7 @@ int sidp_sync(sidp_handle* h) {
   HIPCHK(h, hipMemcpy(&err, h->err, 4, hipMemcpyDeviceToHost));
   if (err) {
     HIPCHK(h, hipMemset(h->err, 0, 4));
-    return SIDP_EINVAL;
+    return err & ~SIDP_DEVERR_NOBLOCKS ? SIDP_EINVAL : SIDP_ENOBLOCKS;
   }
   return SIDP_OK;
 }
@@ -1160,6 +1185,8 @@ int sidp_rope_append(sidp_handle* h, const void* qkv, const int32_t* positions, 
   r.rope_cos = h->rope_cos;
   r.rope_sin = h->rope_sin;
   r.max_seq = h->cfg.max_seq_len;
+  r.rot = h->rope_rot;
+  r.interleaved = h->rope_interleaved;
   r.kv = kv_view(h);
   r.region = region;
   r.q_out = (uint16_t*)q_out;
@@ -1196,6 +1223,155 @@ int sidp_attention(sidp_handle* h, const void* q, int32_t region, const int32_t*
   HIPCHK(h, launch_attention(a, (hipStream_t)stream));
   HIPCHK(h, finish_call(h, (hipStream_t)stream));
   return SIDP_OK;
+}
+
+// ---------------------------------------------------------------- several new tokens a sequence
+
+// Makes the handle's device current for a call and restores the caller's.
+namespace {
+struct OnDevice {
+  int before = -1;
+  hipError_t err;
+  explicit OnDevice(int device) {
+    err = hipGetDevice(&before);
+    if (err == hipSuccess && before != device) err = hipSetDevice(device);
+    else before = -1;
+  }
+  ~OnDevice() {
+    if (before >= 0) (void)hipSetDevice(before);
+  }
+};
+}  // namespace
+
+int sidp_kv_extend(sidp_handle* h, const int32_t* ctx_lens, const int32_t* new_lens, int32_t batch,
+                   const int32_t* free_blocks, int32_t num_free, const int32_t* taken, int32_t* taken_out,
+                   int32_t* block_tables, int32_t max_blocks_per_seq, int32_t max_rows, int32_t* row_starts,
+                   int32_t* positions, int32_t* slots, void* stream) {
+  if (!h || batch < 1 || batch > SIDP_EXTEND_MAX_BATCH || num_free < 0 || max_blocks_per_seq < 1 || max_rows < 0)
+    return SIDP_EINVAL;
+  if (max_blocks_per_seq > (1 << 20) / kBlockTokens || max_rows > SIDP_MAX_ROWS) return SIDP_EINVAL;
+  if (!ctx_lens || !new_lens || !taken || !taken_out || !block_tables || !row_starts) return SIDP_EINVAL;
+  if ((!free_blocks && num_free) || ((!positions || !slots) && max_rows)) return SIDP_EINVAL;
+  if (h->poisoned) return SIDP_ESTATE;
+  ExtendCall c;
+  c.ctx_lens = ctx_lens;
+  c.new_lens = new_lens;
+  c.batch = batch;
+  c.free_blocks = free_blocks;
+  c.num_free = num_free;
+  c.taken = taken;
+  c.taken_out = taken_out;
+  c.block_tables = block_tables;
+  c.max_blocks = max_blocks_per_seq;
+  c.max_rows = max_rows;
+  c.nblk = h->nblk > 0 ? h->nblk : 0x7fffffff / kBlockTokens;
+  c.row_starts = row_starts;
+  c.positions = positions;
+  c.slots = slots;
+  c.err = h->err;
+  const OnDevice on(h->device);
+  HIPCHK(h, on.err);
+  HIPCHK(h, launch_kv_extend(c, (hipStream_t)stream));
+  return SIDP_OK;
+}
+
+int sidp_rope_frequencies(const sidp_rope* rope, int32_t head_dim, double* freqs, double* scale) {
+  if (!rope || !freqs || !scale || (head_dim != 64 && head_dim != 128)) return SIDP_EINVAL;
+  return rope_frequencies(*rope, head_dim, freqs, scale) ? SIDP_OK : SIDP_EINVAL;
+}
+
+int sidp_set_rope(sidp_handle* h, const sidp_rope* rope) {
+  if (!h) return SIDP_EINVAL;
+  double freqs[kMaxPairs], scale;
+  if (rope && !rope_frequencies(*rope, h->cfg.head_dim, freqs, &scale)) return SIDP_EINVAL;
+  if (h->poisoned) return SIDP_ESTATE;
+  const OnDevice on(h->device);
+  HIPCHK(h, on.err);
+  HIPCHK(h, hipDeviceSynchronize());  // no kernel reads the tables while they change
+  if (!rope) return load_default_rope(h);
+  const int e = load_rope(h, freqs, rope->rotary_dim / 2, scale);
+  if (e != SIDP_OK) return e;
+  h->rope_rot = rope->rotary_dim;
+  h->rope_interleaved = rope->layout == SIDP_ROPE_INTERLEAVED;
+  return SIDP_OK;
+}
+
+int sidp_rope_append_rows(sidp_handle* h, const void* qkv, int64_t qkv_stride, int32_t rows, const int32_t* row_count,
+                          const int32_t* positions, const int32_t* slots, const void* g_q, const void* g_k,
+                          int32_t region, void* q_out, void* stream) {
+  if (!h || rows < 0 || rows > SIDP_MAX_ROWS) return SIDP_EINVAL;
+  if (rows > 0 && (!qkv || !positions || !slots || !q_out)) return SIDP_EINVAL;
+  if (qkv_stride < qkv_rows(h->cfg) || qkv_stride % 8) return SIDP_EINVAL;
+  if (((uintptr_t)qkv | (uintptr_t)q_out) % 16) return SIDP_EINVAL;
+  if (h->cfg.qk_norm && (!g_q || !g_k || ((uintptr_t)g_q | (uintptr_t)g_k) % 16)) return SIDP_EINVAL;
+  if (h->poisoned) return SIDP_ESTATE;
+  if (!h->k_cache) return SIDP_ESTATE;
+  if (region < 0 || region >= h->regions) return SIDP_EINVAL;
+  RopeRowsCall r;
+  r.qkv = (const uint16_t*)qkv;
+  r.stride = qkv_stride;
+  r.rows = rows;
+  r.row_count = row_count;
+  r.positions = positions;
+  r.slots = slots;
+  r.hq = h->cfg.num_q_heads;
+  r.hkv = h->cfg.num_kv_heads;
+  r.g_q = h->cfg.qk_norm ? (const uint16_t*)g_q : nullptr;
+  r.g_k = h->cfg.qk_norm ? (const uint16_t*)g_k : nullptr;
+  r.qk_eps = h->cfg.qk_norm_eps;
+  r.rope_cos = h->rope_cos;
+  r.rope_sin = h->rope_sin;
+  r.max_seq = h->cfg.max_seq_len;
+  r.rot = h->rope_rot;
+  r.interleaved = h->rope_interleaved;
+  r.kv = kv_view(h);
+  r.region = region;
+  r.q_out = (uint16_t*)q_out;
+  r.err = h->err;
+  r.num_cus = h->num_cus;
+  const OnDevice on(h->device);
+  HIPCHK(h, on.err);
+  HIPCHK(h, launch_rope_rows(r, (hipStream_t)stream));
+  return SIDP_OK;
+}
+
+// ---------------------------------------------------------------- answers
+
+static bool logprobs_ok(int32_t rows, int32_t vocab, int32_t top_k) {
+  return rows >= 0 && rows <= SIDP_MAX_ROWS && vocab >= 1 && vocab <= SIDP_LOGPROBS_MAX_VOCAB && top_k >= 0 &&
+         top_k <= SIDP_LOGPROBS_MAX_TOP && top_k <= vocab;
+}
+
+size_t sidp_token_logprobs_bytes(int32_t rows, int32_t vocab, int32_t top_k) {
+  if (!logprobs_ok(rows, vocab, top_k) || rows < 1) return 0;
+  return align_up(logprob_ws_bytes(rows, vocab, top_k), kAlign);
+}
+
+int sidp_token_logprobs(const void* logits, int32_t dtype, int32_t rows, int32_t vocab, int64_t row_stride,
+                        const int32_t* targets, int32_t top_k, float* logprobs, int32_t* ranks, float* entropies,
+                        int32_t* top_ids, float* top_logprobs, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!logprobs_ok(rows, vocab, top_k) || row_stride < vocab) return SIDP_EINVAL;
+  if (dtype != SIDP_LOGITS_BF16 && dtype != SIDP_LOGITS_F32) return SIDP_EINVAL;
+  if (rows == 0) return SIDP_OK;
+  if (!logits || (uintptr_t)logits % (dtype == SIDP_LOGITS_F32 ? 4 : 2)) return SIDP_EINVAL;
+  if (top_k > 0 && (!top_ids || !top_logprobs)) return SIDP_EINVAL;
+  if (!workspace || (uintptr_t)workspace % 16 || workspace_bytes < logprob_ws_bytes(rows, vocab, top_k))
+    return SIDP_EINVAL;
+  LogprobCall c;
+  c.logits = logits;
+  c.f32 = dtype == SIDP_LOGITS_F32;
+  c.rows = rows;
+  c.vocab = vocab;
+  c.stride = row_stride;
+  c.targets = targets;
+  c.top = top_k;
+  c.logprob = logprobs;
+  c.rank = ranks;
+  c.entropy = entropies;
+  c.top_ids = top_ids;
+  c.top_logprobs = top_logprobs;
+  c.ws = workspace;
+  return launch_logprobs(c, (hipStream_t)stream) == hipSuccess ? SIDP_OK : SIDP_EHIP;
 }
 
 int sidp_copy(const void* src, void* dst, size_t bytes, int32_t grid, void* stream) {

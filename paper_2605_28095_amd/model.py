@@ -18,6 +18,7 @@ from . import (
     sidp_pool_init,
     sidp_pool_load_layer,
     sidp_set_pooling,
+    sidp_set_rope,
     sidp_sync,
 )
 
@@ -93,6 +94,11 @@ class WaSDecoder:
         """What a streamed layer stages (SIDP_POOL_LAYER / SIDP_POOL_FFN) and which
         layers this rank owns (l % ranks == rank); call between steps, after sync."""
         sidp_set_pooling(self.h, mode, ranks, rank)
+
+    def set_rope(self, rope):
+        """Rotary positions of the steps and single calls from here on (make_rope; None:
+        the config's); call between steps, and before any key is cached."""
+        sidp_set_rope(self.h, rope)
 
     def step(self, hidden, positions, block_tables, flags=SIDP_STREAMED, compute=None, copy=None):
         compute = compute if compute is not None else torch.cuda.current_stream(self.device)
