@@ -565,6 +565,32 @@ int sidp_rope_append_rows(sidp_handle *h, const void *qkv, int64_t qkv_stride, i
                           const int32_t *positions, const int32_t *slots, const void *g_q, const void *g_k,
                           int32_t region, void *q_out, void *stream);
 
+/* Causal paged GQA attention of several new tokens a sequence over region
+ * `region`: for row i of sequence b (position ctx_lens[b] + i) and query head h,
+ * softmax(q K^T / sqrt(D)) V over tokens 0 .. ctx_lens[b] + i of KV head h / (Hq /
+ * Hkv). The rows' own keys and values are in the cache already
+ * (sidp_rope_append_rows).
+ *  q, out       device bf16 [max_rows, Hq, D], 16-byte aligned.
+ *  row_starts   device int32 [batch + 1], as sidp_kv_extend makes them; rows from
+ *               row_starts[batch] on are not touched.
+ *  ctx_lens     device int32 [batch]: tokens cached before the rows.
+ *  block_tables device int32 [batch, max_blocks_per_seq].
+ *  workspace    device, 16-byte aligned, sidp_attention_rows_bytes of the same
+ *               batch and max_rows; nothing in it outlives the call, but calls that
+ *               overlap in time may not share one.
+ * Sequences are cut into runs of keys when there are too few rows to fill the chip,
+ * by the lengths of the whole batch: the last bits of a row can change with the
+ * other rows of the call. A sequence whose rows lie outside max_rows, or whose
+ * tokens outside its table or max_seq_len, latches SIDP_EINVAL and is left out; a
+ * block outside the cache latches it too and counts as zeros. P is rounded to bf16
+ * before it is multiplied with V. batch 1..SIDP_EXTEND_MAX_BATCH. For one new
+ * token a sequence sidp_attention is the call. */
+/* 0 for sizes that sidp_attention_rows refuses, or max_rows 0. */
+size_t sidp_attention_rows_bytes(const sidp_handle *h, int32_t batch, int32_t max_rows);
+int sidp_attention_rows(sidp_handle *h, const void *q, int32_t region, const int32_t *row_starts,
+                        const int32_t *ctx_lens, const int32_t *block_tables, int32_t max_blocks_per_seq, int32_t batch,
+                        int32_t max_rows, void *out, void *workspace, size_t workspace_bytes, void *stream);
+
 /* ---- answers ----
  * Log probabilities of given tokens, their ranks, the entropy and the most likely
  * tokens of each row of logits (the output projection of sidp_linear, say), on the

@@ -55,7 +55,7 @@ EXPORTED = [
     "sidp_timing_collect", "sidp_set_pooling", "sidp_cas_ffn", "sidp_timing_select", "sidp_mode_update",
     "sidp_set_fill_tiles", "sidp_debug_inject_hip_error", "sidp_linear_noalloc", "sidp_linear_plan",
     "sidp_attention_plan", "sidp_kv_extend", "sidp_rope_frequencies", "sidp_set_rope", "sidp_rope_append_rows",
-    "sidp_token_logprobs_bytes", "sidp_token_logprobs",
+    "sidp_attention_rows_bytes", "sidp_attention_rows", "sidp_token_logprobs_bytes", "sidp_token_logprobs",
 ]
 
 SIDP_CAS_MAX_REPLICAS = 16
@@ -160,6 +160,8 @@ _sigs = {
     "sidp_rope_frequencies": (ctypes.c_int, [ctypes.POINTER(sidp_rope), _I, _PD, _PD]),
     "sidp_set_rope": (ctypes.c_int, [_P, ctypes.POINTER(sidp_rope)]),
     "sidp_rope_append_rows": (ctypes.c_int, [_P, _P, ctypes.c_int64, _I, _P, _P, _P, _P, _P, _I, _P, _P]),
+    "sidp_attention_rows_bytes": (_Z, [_P, _I, _I]),
+    "sidp_attention_rows": (ctypes.c_int, [_P, _P, _I, _P, _P, _P, _I, _I, _I, _P, _P, _Z, _P]),
     "sidp_token_logprobs_bytes": (_Z, [_I, _I, _I]),
     "sidp_token_logprobs": (ctypes.c_int, [_P, _I, _I, _I, ctypes.c_int64, _P, _I, _P, _P, _P, _P, _P, _P, _Z, _P]),
     "sidp_copy": (ctypes.c_int, [_P, _P, _Z, _I, _P]),
@@ -448,6 +450,17 @@ def sidp_rope_append_rows(h, qkv, qkv_stride, rows, row_count, positions, slots,
     _check(_lib.sidp_rope_append_rows(h, _ptr(qkv), qkv_stride, rows, _ptr(row_count), _ptr(positions), _ptr(slots),
                                       _ptr(g_q), _ptr(g_k), region, _ptr(q_out), _stream(stream)),
            "sidp_rope_append_rows")
+
+
+def sidp_attention_rows_bytes(h, batch, max_rows):
+    return _lib.sidp_attention_rows_bytes(h, batch, max_rows)
+
+
+def sidp_attention_rows(h, q, region, row_starts, ctx_lens, block_tables, max_blocks_per_seq, batch, max_rows, out,
+                        workspace, workspace_bytes, stream=None):
+    _check(_lib.sidp_attention_rows(h, _ptr(q), region, _ptr(row_starts), _ptr(ctx_lens), _ptr(block_tables),
+                                    max_blocks_per_seq, batch, max_rows, _ptr(out), _ptr(workspace), workspace_bytes,
+                                    _stream(stream)), "sidp_attention_rows")
 
 
 def sidp_token_logprobs_bytes(rows, vocab, top_k):

@@ -200,6 +200,24 @@ hipError_t launch_attn_plan(const AttnCall& c, hipStream_t s);
 hipError_t launch_attention(const AttnCall& c, hipStream_t s, hipEvent_t start = nullptr,
                             hipEvent_t stop = nullptr);
 
+// Several new tokens a sequence: see sidp_attention_rows.
+struct AttnRowsCall {
+  const uint16_t* q;  // [rows][Hq][D]
+  const int32_t* row_starts;
+  const int32_t* ctx_lens;
+  const int32_t* block_tables;
+  int max_blocks, batch, max_rows, max_seq;
+  int hq;
+  KvView kv;
+  int region;
+  uint16_t* out;
+  void* ws;
+  uint32_t* err;
+  int num_cus;
+};
+size_t attn_rows_ws_bytes(int batch, int max_rows, int hq, int hkv, int d, int max_seq, int num_cus);
+hipError_t launch_attention_rows(const AttnRowsCall& c, hipStream_t s);
+
 hipError_t launch_copy(const void* src, void* dst, size_t bytes, int grid, hipStream_t s);
 
 // Rows moved between per-replica buffers and one contiguous staging buffer:

@@ -1335,6 +1335,50 @@ int sidp_rope_append_rows(sidp_handle* h, const void* qkv, int64_t qkv_stride, i
   return SIDP_OK;
 }
 
+static bool attention_rows_ok(int32_t batch, int32_t max_rows) {
+  return batch >= 1 && batch <= SIDP_EXTEND_MAX_BATCH && max_rows >= 0 && max_rows <= SIDP_MAX_ROWS;
+}
+
+size_t sidp_attention_rows_bytes(const sidp_handle* h, int32_t batch, int32_t max_rows) {
+  if (!h || !attention_rows_ok(batch, max_rows) || max_rows < 1) return 0;
+  const sidp_config& c = h->cfg;
+  return attn_rows_ws_bytes(batch, max_rows, c.num_q_heads, c.num_kv_heads, c.head_dim, c.max_seq_len, h->num_cus);
+}
+
+int sidp_attention_rows(sidp_handle* h, const void* q, int32_t region, const int32_t* row_starts,
+                        const int32_t* ctx_lens, const int32_t* block_tables, int32_t max_blocks_per_seq, int32_t batch,
+                        int32_t max_rows, void* out, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!h || !attention_rows_ok(batch, max_rows) || max_blocks_per_seq < 1) return SIDP_EINVAL;
+  if (max_blocks_per_seq > (1 << 20) / kBlockTokens) return SIDP_EINVAL;
+  if (h->poisoned) return SIDP_ESTATE;
+  if (!h->k_cache) return SIDP_ESTATE;
+  if (region < 0 || region >= h->regions) return SIDP_EINVAL;
+  if (max_rows == 0) return SIDP_OK;
+  if (!q || !row_starts || !ctx_lens || !block_tables || !out || !workspace) return SIDP_EINVAL;
+  if (((uintptr_t)q | (uintptr_t)out | (uintptr_t)workspace) % 16) return SIDP_EINVAL;
+  if (workspace_bytes < sidp_attention_rows_bytes(h, batch, max_rows)) return SIDP_EINVAL;
+  AttnRowsCall a;
+  a.q = (const uint16_t*)q;
+  a.row_starts = row_starts;
+  a.ctx_lens = ctx_lens;
+  a.block_tables = block_tables;
+  a.max_blocks = max_blocks_per_seq;
+  a.batch = batch;
+  a.max_rows = max_rows;
+  a.max_seq = h->cfg.max_seq_len;
+  a.hq = h->cfg.num_q_heads;
+  a.kv = kv_view(h);
+  a.region = region;
+  a.out = (uint16_t*)out;
+  a.ws = workspace;
+  a.err = h->err;
+  a.num_cus = h->num_cus;
+  const OnDevice on(h->device);
+  HIPCHK(h, on.err);
+  HIPCHK(h, launch_attention_rows(a, (hipStream_t)stream));
+  return SIDP_OK;
+}
+
 // ---------------------------------------------------------------- answers
 
 static bool logprobs_ok(int32_t rows, int32_t vocab, int32_t top_k) {
