@@ -11,13 +11,16 @@
 // so a pair's scores lie in two lanes and its softmax needs one exchange between
 // them. The tokens of S^T's rows are permuted (bits 2 and 3 of a token's place in
 // its block change places) so that the eight probabilities a lane needs for the
-// second product are the ones it computed. Softmax is online in base-2 units; the
-// reference only moves when a score is more than 2^kLazy above it (fp32 sums have
-// the room), which leaves the accumulators alone in most chunks.
+// second product are the ones it computed. Softmax is online in base-2 units. Its
+// reference is a score of the pair, not always the largest: it only moves when a
+// chunk's weights sum to more than kMost (fp32 and bf16 have the range), so that
+// most chunks need no maximum and leave the accumulators alone.
 //
 // P is rounded to bf16 for the second product: at most 2^-8 relative and independent from
 // key to key, so the sum is off by no more than its own rounding to bf16; the
 // sum of P is fp32 and unrounded.
+#include <type_traits>
+
 #include "common.h"
 #include "internal.h"
 
@@ -26,15 +29,17 @@ namespace sidp {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr int kChunk = 64;        // tokens staged at a time
+constexpr int kChunk = 32;        // tokens staged at a time
+constexpr int kRing = 4;          // chunks of K, and of V, in LDS
 constexpr int kChunkBlocks = kChunk / kBlockTokens;
-constexpr float kLazy = 8.f;
+constexpr float kMost = 4096.f;
 constexpr int kWaves = 4;
+constexpr int kTileRows = 32 * kWaves;  // (token, head) pairs of a tile
 
 // Items (entry, KV head) the chip holds at once: two workgroups a CU.
 constexpr int kSlotsPerCu = 2;
 // A launch with fewer items than slots cuts sequences into runs of at least this many chunks.
-constexpr int kMinRun = 8;
+constexpr int kMinRun = 16;
 
 typedef const __attribute__((address_space(4))) int32_t cint32_t;
 
@@ -224,27 +229,29 @@ __device__ __forceinline__ uint32_t keep_finite(uint32_t v) {
 __device__ __forceinline__ bool any_not_finite(uint32_t v) {
   return (v & 0x7f80u) == 0x7f80u || (v & 0x7f800000u) == 0x7f800000u;
 }
-// bf16 ones where the value is +inf (which 0), -inf (1), NaN (2)
-__device__ __forceinline__ uint32_t ones_where(uint32_t v, int which) {
-  auto is = [&](uint32_t h) {
-    return which == 0 ? h == 0x7f80u : which == 1 ? h == 0xff80u : (h & 0x7fffu) > 0x7f80u;
-  };
-  return (is(v & 0xffffu) ? 0x3f80u : 0u) | (is(v >> 16) ? 0x3f800000u : 0u);
+// 16 bytes a lane, straight to LDS: lane l's land at dst + 16 l.
+__device__ __forceinline__ void load_lds16(const char* src, char* dst) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
+                                   (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
 }
 
-// NR: 32-pair column sets of a wave.
-template <int D, int NR>
-__global__ void __launch_bounds__(256, NR == 1 ? 2 : 1) k_attn_rows(AttnRowsCall c, Layout lay) {
+// The larger of a lane's value and its counterpart's in the other half of the wave.
+__device__ __forceinline__ float max_halves(float v) {
+  const u32x2_t r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+template <int D>
+__global__ void __launch_bounds__(256, 2) k_attn_rows(AttnRowsCall c, Layout lay) {
   constexpr int KK = D / 16, DT = D / 32;
   constexpr int kBlockBytes = kBlockTokens * D * 2;
-  constexpr int kHalf = D * 16 + 128;  // V block in LDS: [token / 8][d][token % 8], halves 128 bytes apart in the banks
-  constexpr int kVBlock = 2 * kHalf;
-  constexpr int kKBytes = kChunkBlocks * kBlockBytes, kBuf = kKBytes + kChunkBlocks * kVBlock;
-  constexpr int kPieces = kKBytes / 16 / 256;  // 16-byte pieces of K (and of V) that a thread stages
-  constexpr int kPerBlock = kBlockBytes / 16;
-  constexpr int kTileRows = 32 * NR * kWaves;
-  extern __shared__ __attribute__((aligned(16))) char smem[];  // two buffers
-  __shared__ int s_flag[2];
+  constexpr int kSide = kChunkBlocks * kBlockBytes;  // K or V of a chunk
+  constexpr int kBlockWaves = D / 32;                // waves that load a block's K (and V), 16 bytes a lane
+  constexpr int kPieces = kChunkBlocks * kBlockWaves / kWaves;
+  constexpr int kGroupChunks = 64 / kChunkBlocks;    // chunks whose block ids a wave holds, one a lane
+  extern __shared__ __attribute__((aligned(16))) char smem[];  // the rings of K and of V
+  __shared__ int s_odd;          // whether an edge chunk held values that are not finite
+  __shared__ int s_first[3][D];  // and the first tokens that hold +inf, -inf and NaN, of each dim
 
   const int t = threadIdx.x, lane = t & 63, col = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
@@ -259,244 +266,280 @@ __global__ void __launch_bounds__(256, NR == 1 ? 2 : 1) k_attn_rows(AttnRowsCall
   const int tokens = min(tm, ((cint32_t*)c.row_starts)[b + 1] - row0);  // of this tile
   const int first_pos = ((cint32_t*)c.ctx_lens)[b] + tile * tm;         // of its first row
   const int kv_end = first_pos + tokens;
-  cint32_t* bt = (cint32_t*)(c.block_tables + (int64_t)b * c.max_blocks);
-  const int64_t region_blk = (int64_t)c.region * c.kv.nblk;
+  const int blocks = (kv_end + kBlockTokens - 1) / kBlockTokens;
+  const int32_t* bt = c.block_tables + (int64_t)b * c.max_blocks;
   const float scale = kLog2e / sqrtf((float)D);
-  if (t < 2) s_flag[t] = -1;
+  if (t == 0) s_odd = 0;
+  for (int i = t; i < 3 * D; i += 256) (&s_first[0][0])[i] = 0x7fffffff;
 
-  // this lane's pairs, their queries, and the keys they see
-  bf16x8_t q[NR][KK];
-  int limit[NR];
-  int64_t out_row[NR];
+  // this lane's pair, its query, and the keys it sees
+  const int pair = wave * 32 + col;
+  const int tok = pair / group, head = pair - tok * group;
+  const bool live = tok < tokens;  // pairs past tm * group have tok >= tm
+  const int limit = live ? first_pos + tok + 1 : 0;
+  bf16x8_t q[KK];
+  {
+    const uint16_t* qp = c.q + ((int64_t)(row0 + (live ? tok : 0)) * c.hq + g * group + (live ? head : 0)) * D + half * 8;
 #pragma unroll
-  for (int n = 0; n < NR; n++) {
-    const int pair = (wave * NR + n) * 32 + col;
-    const int tok = pair / group, head = pair - tok * group;
-    const bool live = tok < tokens;  // pairs past tm * group have tok >= tm
-    limit[n] = live ? first_pos + tok + 1 : 0;
-    out_row[n] = live ? (int64_t)(row0 + tok) * c.hq + g * group + head : -1;
-    const uint16_t* qp = c.q + (live ? out_row[n] : (int64_t)row0 * c.hq + g * group) * D + half * 8;
-#pragma unroll
-    for (int kk = 0; kk < KK; kk++) q[n][kk] = as_bf16x8(*(const u32x4_t*)(qp + kk * 16));
+    for (int kk = 0; kk < KK; kk++) q[kk] = as_bf16x8(*(const u32x4_t*)(qp + kk * 16));
   }
   // pairs of a wave are in token order: the fewest and the most keys that its pairs see
-  const int wave_first = wave * NR * 32 / group;
+  const int wave_first = wave * 32 / group;
   const bool wave_live = wave_first < tokens;
   const int wave_least = first_pos + wave_first + 1;
-  const int wave_most = first_pos + min(tokens, (wave * NR * 32 + NR * 32 - 1) / group + 1);
+  const int wave_most = wave_live ? first_pos + min(tokens, (wave * 32 + 31) / group + 1) : 0;
 
-  f32x16_t o[NR][DT];
-  float m_ref[NR], l[NR];
+  f32x16_t o[DT];
+  float m_ref = live ? -INFINITY : 0.f, l = 0.f;
 #pragma unroll
-  for (int n = 0; n < NR; n++) {
-    m_ref[n] = -INFINITY;
-    l[n] = 0.f;
+  for (int dt = 0; dt < DT; dt++)
 #pragma unroll
-    for (int dt = 0; dt < DT; dt++)
-#pragma unroll
-      for (int r = 0; r < 16; r++) o[n][dt][r] = 0.f;
-  }
+    for (int r = 0; r < 16; r++) o[dt][r] = 0.f;
 
-  u32x4_t sk[kPieces], sv[kPieces];
+  // Block ids of 32 chunks, one a lane, and of the 32 behind them (loaded a group
+  // ahead: a wait for an id would wait for the chunks in flight too). A block
+  // outside the cache is read as block 0, places past the last block as the last.
   bool bad = false;
-  // Loads chunk `ch` into registers; blocks past kv_end are zeros, as is the V of tokens past it (anything may stand there).
-  auto load = [&](int ch) {
+  auto load_ids = [&](int chunk) { return bt[min(chunk * kChunkBlocks + lane, blocks - 1)]; };
+  auto checked = [&](int id) {
+    const bool ok = id >= 0 && id < c.kv.nblk;
+    bad |= !ok;
+    return ok ? id : 0;
+  };
+  int ids_k = checked(load_ids(c0)), ids_next = load_ids(c0 + kGroupChunks), ids_v = ids_k;  // V is fetched two chunks later
+  const int64_t region_blk = (int64_t)c.region * c.kv.nblk;
+  const int blk_wave = wave / kBlockWaves, in_block = wave % kBlockWaves;
+  // K blocks go to LDS as they are; V blocks as [token / 8][d][token % 8], so that 32 dims' pieces are contiguous
+  const uint32_t k_src = (in_block * 64 + lane) * 16;
+  const uint32_t v_src = (in_block % (kBlockWaves / 2) * 64 + lane) * 32 + in_block / (kBlockWaves / 2) * 16;
+  auto fetch = [&](int ch, int ids, const void* cache, uint32_t src, char* ring) {
 #pragma unroll
     for (int j = 0; j < kPieces; j++) {
-      const int blk_in = kPerBlock >= 256 ? j : __builtin_amdgcn_readfirstlane(j * (256 / kPerBlock) + t / kPerBlock);
-      const int piece = kPerBlock >= 256 ? t : t % kPerBlock;
-      const int t0 = ch * kChunk + blk_in * kBlockTokens;
-      sk[j] = sv[j] = u32x4_t{0, 0, 0, 0};
-      if (t0 < kv_end) {
-        const int blk = bt[t0 / kBlockTokens];
-        if (blk >= 0 && blk < c.kv.nblk) {
-          const int64_t off = ((region_blk + blk) * hkv + g) * (int64_t)kBlockBytes + piece * 16;
-          sk[j] = *(const u32x4_t*)((const char*)c.kv.k + off);
-          sv[j] = *(const u32x4_t*)((const char*)c.kv.v + off);
-        } else {
-          bad = true;
-        }
-      }
+      const int in_chunk = j * (kWaves / kBlockWaves) + blk_wave;
+      const int blk = __builtin_amdgcn_readlane(ids, (ch - c0) % kGroupChunks * kChunkBlocks + in_chunk);
+      load_lds16((const char*)cache + ((region_blk + blk) * hkv + g) * (int64_t)kBlockBytes + src,
+                 ring + (ch - c0) % kRing * kSide + in_chunk * kBlockBytes + in_block * 1024);
     }
   };
-  // The V checks: only a chunk that the tile's first row does not see whole can hold masked tokens.
-  auto store = [&](int ch, int buf) {
-    char* kb = smem + buf * kBuf;
-    char* vb = kb + kKBytes;
-    const bool edge = (ch + 1) * kChunk > first_pos + 1;
-#pragma unroll
-    for (int j = 0; j < kPieces; j++) {
-      const int blk_in = kPerBlock >= 256 ? j : j * (256 / kPerBlock) + t / kPerBlock;
-      const int piece = kPerBlock >= 256 ? t : t % kPerBlock;
-      if (edge) {
-        const int t0 = ch * kChunk + blk_in * kBlockTokens + (piece & 1) * 8;
-        bool odd = false;
-#pragma unroll
-        for (int i = 0; i < 4; i++) {
-          if (t0 + 2 * i >= kv_end) sv[j][i] = 0;
-          else if (t0 + 2 * i + 1 >= kv_end) sv[j][i] &= 0xffffu;
-          odd |= any_not_finite(sv[j][i]);
-        }
-        if (odd) s_flag[buf] = ch;
-      }
-      *(u32x4_t*)(kb + blk_in * kBlockBytes + piece * 16) = sk[j];
-      *(u32x4_t*)(vb + blk_in * kVBlock + (piece & 1) * kHalf + (piece >> 1) * 16) = sv[j];
+  auto fetch_k = [&](int ch) {
+    if (ch >= c1) return;
+    if (ch > c0 && (ch - c0) % kGroupChunks == 0) {
+      ids_k = checked(ids_next);
+      ids_next = load_ids(ch + kGroupChunks);
     }
+    fetch(ch, ids_k, c.kv.k, k_src, smem);
+  };
+  auto fetch_v = [&](int ch) {
+    if (ch >= c1) return;
+    if ((ch - c0) % kGroupChunks == 0) ids_v = ids_k;
+    fetch(ch, ids_v, c.kv.v, v_src, smem + kRing * kSide);
+  };
+  // Waits until this wave's loads but the last 4 * kPieces have landed (all, with `all`), then for the other waves.
+  auto landed = [&](bool all) {
+    if (all) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    else asm volatile("s_waitcnt vmcnt(%0)" ::"n"(4 * kPieces) : "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
+  // The V of an edge chunk (one that the tile's first row does not see whole), landed. Tokens past kv_end become zeros (anything
+  // may stand there). So do values that are not finite, for 0 * inf would reach the rows that do not see them: they are added to
+  // the others at the end, where an inf or a NaN is an inf or a NaN whenever it came.
+  auto mend = [&](int ch) {
+    if ((ch + 1) * kChunk <= first_pos + 1) return;
+    char* vb = smem + (kRing + (ch - c0) % kRing) * kSide;
+    for (int i = t; i < kSide / 16; i += 256) {
+      const int t0 = ch * kChunk + i / (2 * D) * kBlockTokens + i / D % 2 * 8;
+      u32x4_t v = *(const u32x4_t*)(vb + i * 16);
+#pragma unroll
+      for (int k = 0; k < 4; k++) {
+        if (t0 + 2 * k >= kv_end) v[k] = 0;
+        else if (t0 + 2 * k + 1 >= kv_end) v[k] &= 0xffffu;
+      }
+      if (any_not_finite(v[0]) || any_not_finite(v[1]) || any_not_finite(v[2]) || any_not_finite(v[3])) {
+        s_odd = 1;
+        for (int k = 0; k < 8; k++) {
+          const uint32_t h = (k & 4 ? (k & 2 ? v[3] : v[2]) : (k & 2 ? v[1] : v[0])) >> 16 * (k & 1) & 0xffffu;
+          if ((h & 0x7f80u) == 0x7f80u) atomicMin(&s_first[h == 0x7f80u ? 0 : h == 0xff80u ? 1 : 2][i % D], t0 + k);
+        }
+#pragma unroll
+        for (int k = 0; k < 4; k++) v[k] = keep_finite(v[k]);
+      }
+      *(u32x4_t*)(vb + i * 16) = v;
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
   };
 
-  __syncthreads();
-  load(c0);
-  store(c0, 0);
-  __syncthreads();
   // K: the token of S^T's row m is m with bits 2 and 3 exchanged
   const int ktok = (col & 3) | ((col >> 2) & 1) << 3 | ((col >> 3) & 1) << 2;
-  const int k_lane = (col >> 4) * kBlockBytes + (half * 16 + ktok) * 16;
-  const int v_lane = half * kHalf + col * 16;
-  for (int ch = c0; ch < c1; ch++) {
-    const int buf = (ch - c0) & 1;
-    if (ch + 1 < c1) load(ch + 1);
-    const char* kb = smem + buf * kBuf;
-    const char* vb = kb + kKBytes;
-    const int t0 = ch * kChunk;
-    if (wave_live && t0 < wave_most) {
-      f32x16_t s[NR][2];
+  const uint32_t k_lane = (col >> 4) * kBlockBytes + (half * 16 + ktok) * 16;
+  const uint32_t v_lane = half * (D * 16) + col * 16;
+  auto scores = [&](int ch, f32x16_t& s) {
+    const char* kb = smem + (ch - c0) % kRing * kSide + k_lane;
 #pragma unroll
-      for (int n = 0; n < NR; n++)
+    for (int r = 0; r < 16; r++) s[r] = 0.f;
 #pragma unroll
-        for (int tt = 0; tt < 2; tt++)
+    for (int kk = 0; kk < KK; kk++)
+      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(*(const u32x4_t*)(kb + kk * 512)), q[kk], s, 0, 0, 0);
+  };
+  // Register r: token 16 (r / 8) + 8 half + r % 8 of the chunk.
+  auto mask = [&](int ch, f32x16_t& s) {
+    if ((ch + 1) * kChunk > wave_least) {
 #pragma unroll
-          for (int r = 0; r < 16; r++) s[n][tt][r] = 0.f;
-#pragma unroll
-      for (int kk = 0; kk < KK; kk++)
-#pragma unroll
-        for (int tt = 0; tt < 2; tt++) {
-          const bf16x8_t kf = as_bf16x8(*(const u32x4_t*)(kb + tt * 2 * kBlockBytes + kk * 512 + k_lane));
-#pragma unroll
-          for (int n = 0; n < NR; n++) s[n][tt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[n][kk], s[n][tt], 0, 0, 0);
-        }
-      const bool edge = t0 + kChunk > wave_least;
-      bf16x8_t p[NR][4];
-      uint32_t seen[NR];  // edge: whether the pair sees the token of each of its 32 scores
-#pragma unroll
-      for (int n = 0; n < NR; n++) {
-        // register r of S^T's tile tt holds token 32 tt + 16 (r / 8) + 8 half + r % 8
-        if (edge) {
-          seen[n] = 0;
-#pragma unroll
-          for (int tt = 0; tt < 2; tt++)
-#pragma unroll
-            for (int r = 0; r < 16; r++) {
-              const bool sees = t0 + 32 * tt + 16 * (r / 8) + 8 * half + r % 8 < limit[n];
-              seen[n] |= (uint32_t)sees << (16 * tt + r);
-              s[n][tt][r] = sees ? s[n][tt][r] : -INFINITY;
-            }
-        }
-        float cm = s[n][0][0];
-#pragma unroll
-        for (int tt = 0; tt < 2; tt++)
-#pragma unroll
-          for (int r = 0; r < 16; r++) cm = fmaxf(cm, s[n][tt][r]);
-        cm = fmaxf(cm, __shfl_xor(cm, 32, 64)) * scale;
-        if (__any(cm > m_ref[n] + kLazy)) {
-          const float m_new = fmaxf(m_ref[n], cm);
-          const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_ref[n] - m_new);
-          m_ref[n] = m_new;
-          l[n] *= alpha;
-#pragma unroll
-          for (int dt = 0; dt < DT; dt++)
-#pragma unroll
-            for (int r = 0; r < 16; r++) o[n][dt][r] *= alpha;
-        }
-        const float base = m_ref[n] == -INFINITY ? 0.f : -m_ref[n];
-        float sum = 0.f;
-#pragma unroll
-        for (int tt = 0; tt < 2; tt++) {
-#pragma unroll
-          for (int r = 0; r < 16; r++) {
-            const float e = __builtin_amdgcn_exp2f(fmaf(s[n][tt][r], scale, base));
-            s[n][tt][r] = e;
-            sum += e;
-          }
-#pragma unroll
-          for (int k = 0; k < 2; k++)
-            p[n][2 * tt + k] = as_bf16x8(u32x4_t{pack_bf2(s[n][tt][8 * k], s[n][tt][8 * k + 1]), pack_bf2(s[n][tt][8 * k + 2], s[n][tt][8 * k + 3]),
-                                                 pack_bf2(s[n][tt][8 * k + 4], s[n][tt][8 * k + 5]), pack_bf2(s[n][tt][8 * k + 6], s[n][tt][8 * k + 7])});
-        }
-        l[n] += sum;
-      }
-      if (edge && s_flag[buf] == ch) {
-        // Values that are not finite, beside tokens that some pairs do not see: 0 * inf would reach those pairs. The finite
-        // ones are multiplied as ever; the others are added where a pair sees them.
-#pragma unroll
-        for (int k = 0; k < 4; k++)
-#pragma unroll
-          for (int dt = 0; dt < DT; dt++) {
-            const u32x4_t v = *(const u32x4_t*)(vb + k * kVBlock + v_lane + dt * 512);
-            const bf16x8_t vf = as_bf16x8(u32x4_t{keep_finite(v[0]), keep_finite(v[1]), keep_finite(v[2]), keep_finite(v[3])});
-#pragma unroll
-            for (int n = 0; n < NR; n++) {
-              o[n][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, p[n][k], o[n][dt], 0, 0, 0);
-              uint32_t w[4];
-#pragma unroll
-              for (int i = 0; i < 4; i++) {
-                const uint32_t two = seen[n] >> (8 * k + 2 * i);
-                w[i] = (two & 1u ? 0x3f80u : 0u) | (two & 2u ? 0x3f800000u : 0u);
-              }
-              const bf16x8_t sees = as_bf16x8(u32x4_t{w[0], w[1], w[2], w[3]});
-              for (int which = 0; which < 3; which++) {
-                const bf16x8_t of = as_bf16x8(u32x4_t{ones_where(v[0], which), ones_where(v[1], which), ones_where(v[2], which), ones_where(v[3], which)});
-                f32x16_t cnt;
-#pragma unroll
-                for (int r = 0; r < 16; r++) cnt[r] = 0.f;
-                cnt = __builtin_amdgcn_mfma_f32_32x32x16_bf16(of, sees, cnt, 0, 0, 0);
-                const float add = which == 0 ? INFINITY : which == 1 ? -INFINITY : NAN;
-#pragma unroll
-                for (int r = 0; r < 16; r++)
-                  if (cnt[r] > 0.f) o[n][dt][r] += add;
-              }
-            }
-          }
-      } else {
-#pragma unroll
-        for (int k = 0; k < 4; k++)
-#pragma unroll
-          for (int dt = 0; dt < DT; dt++) {
-            const bf16x8_t vf = as_bf16x8(*(const u32x4_t*)(vb + k * kVBlock + v_lane + dt * 512));
-#pragma unroll
-            for (int n = 0; n < NR; n++) o[n][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, p[n][k], o[n][dt], 0, 0, 0);
-          }
-      }
+      for (int r = 0; r < 16; r++) s[r] = ch * kChunk + 16 * (r / 8) + 8 * half + r % 8 < limit ? s[r] : -INFINITY;
     }
-    if (ch + 1 < c1) store(ch + 1, buf ^ 1);
-    __syncthreads();
+  };
+  // The weights of a chunk's keys against the reference as it is, and their sum.
+  auto weights = [&](const f32x16_t& s, bf16x8_t (&p)[2]) {
+    const float base = m_ref == -INFINITY ? 0.f : -m_ref;
+    float sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < 2; k++) {
+      float e[8];
+#pragma unroll
+      for (int r = 0; r < 8; r++) {
+        e[r] = __builtin_amdgcn_exp2f(fmaf(s[8 * k + r], scale, base));
+        sum += e[r];
+      }
+      p[k] = as_bf16x8(u32x4_t{pack_bf2(e[0], e[1]), pack_bf2(e[2], e[3]), pack_bf2(e[4], e[5]), pack_bf2(e[6], e[7])});
+    }
+    return sum;
+  };
+  // Moves the reference to the chunk's largest score where the weights have grown too large for the one they had.
+  auto weigh = [&](const f32x16_t& s, bf16x8_t (&p)[2], float sum) {
+    if (__any(sum > kMost || m_ref == -INFINITY)) {
+      float cm = s[0];
+#pragma unroll
+      for (int r = 1; r < 16; r++) cm = fmaxf(cm, s[r]);
+      const float m_new = fmaxf(m_ref, max_halves(cm) * scale);
+      const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_ref - m_new);
+      m_ref = m_new;
+      l *= alpha;
+#pragma unroll
+      for (int dt = 0; dt < DT; dt++)
+#pragma unroll
+        for (int r = 0; r < 16; r++) o[dt][r] *= alpha;
+      sum = weights(s, p);
+    }
+    l += sum;
+  };
+  auto add_values = [&](int ch, const bf16x8_t (&p)[2]) {
+    const char* vb = smem + (kRing + (ch - c0) % kRing) * kSide + v_lane;
+#pragma unroll
+    for (int k = 0; k < 2; k++)
+#pragma unroll
+      for (int dt = 0; dt < DT; dt++)
+        o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(*(const u32x4_t*)(vb + k * kBlockBytes + dt * 512)), p[k], o[dt],
+                                                        0, 0, 0);
+  };
+  // A turn makes chunk ch's weights on the vector units while the matrix units add chunk ch - 1's values and make chunk ch + 1's
+  // scores: at its start V(ch - 1) and K(ch + 1) have landed, and V(ch + 2) and K(ch + 4) are fetched into the places of V(ch - 2)
+  // and K(ch), three turns before their use. (Behind the last chunk the scores are of whatever lies there, and nobody's.)
+  auto turn = [&](auto first, int ch, f32x16_t& s, f32x16_t& s_next, bf16x8_t (&p_last)[2], bf16x8_t (&p)[2]) {
+    constexpr bool kFirst = decltype(first)::value;
+    fetch_v(ch + 2);
+    fetch_k(ch + 4);
+    if (ch * kChunk < wave_most) {
+      mask(ch, s);
+      // Products take turns between the two, each with its share of the weights' arithmetic behind it, and fragments are read
+      // kAhead products ahead.
+      constexpr int kProducts = KK + (kFirst ? 0 : 2 * DT), kShare = 16 / kProducts, kAhead = 3;
+      const char* kb = smem + (ch + 1 - c0) % kRing * kSide + k_lane;
+      const char* vb = smem + (kRing + (ch + kRing - 1 - c0) % kRing) * kSide + v_lane;
+      u32x4_t frag[kAhead + 1];
+      auto read = [&](int i) {
+        const char* from = kFirst ? kb + i * 512 : i % 2 ? kb + i / 2 * 512 : vb + i / 2 / DT * kBlockBytes + i / 2 % DT * 512;
+        frag[i % (kAhead + 1)] = *(const u32x4_t*)from;
+      };
+      const float base = m_ref == -INFINITY ? 0.f : -m_ref;
+      float sum = 0.f, e[16];
+#pragma unroll
+      for (int r = 0; r < 16; r++) s_next[r] = 0.f;
+#pragma unroll
+      for (int i = 0; i < kAhead; i++) read(i);
+#pragma unroll
+      for (int i = 0; i < kProducts; i++) {
+        __builtin_amdgcn_sched_barrier(0);
+        if (i + kAhead < kProducts) read(i + kAhead);
+        const bf16x8_t f = as_bf16x8(frag[i % (kAhead + 1)]);
+        if (kFirst || i % 2) s_next = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, q[kFirst ? i : i / 2], s_next, 0, 0, 0);
+        else o[i / 2 % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, p_last[i / 2 / DT], o[i / 2 % DT], 0, 0, 0);
+#pragma unroll
+        for (int r = i * kShare; r < (i + 1) * kShare; r++) {
+          e[r] = __builtin_amdgcn_exp2f(fmaf(s[r], scale, base));
+          if (r > 0) sum += e[r - 1];  // a step late: nothing waits for the exponential
+          if (r % 8 == 7) {
+            const float* w = e + r - 7;
+            p[r / 8] = as_bf16x8(u32x4_t{pack_bf2(w[0], w[1]), pack_bf2(w[2], w[3]), pack_bf2(w[4], w[5]), pack_bf2(w[6], w[7])});
+          }
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      sum += e[15];
+      weigh(s, p, sum);
+    } else if (!kFirst && (ch - 1) * kChunk < wave_most) {
+      add_values(ch - 1, p_last);
+    }
+    landed(ch + 4 >= c1);
+    mend(ch);
+  };
+  f32x16_t sa, sb;
+  bf16x8_t pa[2], pb[2];
+  fetch_k(c0);
+  fetch_k(c0 + 1);
+  fetch_v(c0);
+  fetch_k(c0 + 2);
+  fetch_v(c0 + 1);
+  fetch_k(c0 + 3);
+  landed(c0 + 4 > c1);
+  if (c0 * kChunk < wave_most) scores(c0, sa);
+  __builtin_amdgcn_s_barrier();  // K(c0) is read
+  asm volatile("" ::: "memory");
+  turn(std::true_type{}, c0, sa, sb, pb, pa);
+  for (int ch = c0 + 1; ch < c1; ch += 2) {
+    turn(std::false_type{}, ch, sb, sa, pa, pb);
+    if (ch + 1 < c1) turn(std::false_type{}, ch + 1, sa, sb, pb, pa);
+  }
+  if ((c1 - 1) * kChunk < wave_most) {
+    if ((c1 - c0) & 1) add_values(c1 - 1, pa);
+    else add_values(c1 - 1, pb);
   }
   if (bad) atomicOr(c.err, SIDP_DEVERR_BLOCK);
 
   // Register r of O^T's tile dt is dim 32 dt + 8 (r / 4) + 4 half + r % 4.
+  if (s_odd) {
 #pragma unroll
-  for (int n = 0; n < NR; n++) {
-    const float sum = l[n] + __shfl_xor(l[n], 32, 64);
-    if (out_row[n] < 0) continue;
-    if (rec < 0) {
-      const float inv = 1.f / sum;
-      uint16_t* op = c.out + out_row[n] * D + half * 4;
+    for (int dt = 0; dt < DT; dt++)
 #pragma unroll
-      for (int dt = 0; dt < DT; dt++)
+      for (int r = 0; r < 16; r++) {
+        const int d = 32 * dt + 8 * (r / 4) + 4 * half + r % 4;
+        if (s_first[0][d] < limit) o[dt][r] += INFINITY;
+        if (s_first[1][d] < limit) o[dt][r] -= INFINITY;
+        if (s_first[2][d] < limit) o[dt][r] = NAN;
+      }
+  }
+  const float sum = l + __shfl_xor(l, 32, 64);
+  if (!live) return;
+  const int64_t out_row = (int64_t)(row0 + tok) * c.hq + g * group + head;
+  if (rec < 0) {
+    const float inv = 1.f / sum;
+    uint16_t* op = c.out + out_row * D + half * 4;
 #pragma unroll
-        for (int i = 0; i < 4; i++)
-          *(u32x2_t*)(op + dt * 32 + i * 8) = u32x2_t{pack_bf2(o[n][dt][4 * i] * inv, o[n][dt][4 * i + 1] * inv),
-                                                      pack_bf2(o[n][dt][4 * i + 2] * inv, o[n][dt][4 * i + 3] * inv)};
-    } else {
-      const int pair = (wave * NR + n) * 32 + col;
-      float* r = (float*)((char*)c.ws + lay.recs) + ((int64_t)rec * hkv + g) * lay.rec_rows * (D + 2);
+    for (int dt = 0; dt < DT; dt++)
 #pragma unroll
-      for (int dt = 0; dt < DT; dt++)
+      for (int i = 0; i < 4; i++)
+        *(u32x2_t*)(op + dt * 32 + i * 8) = u32x2_t{pack_bf2(o[dt][4 * i] * inv, o[dt][4 * i + 1] * inv),
+                                                    pack_bf2(o[dt][4 * i + 2] * inv, o[dt][4 * i + 3] * inv)};
+  } else {
+    float* r = (float*)((char*)c.ws + lay.recs) + ((int64_t)rec * hkv + g) * lay.rec_rows * (D + 2);
 #pragma unroll
-        for (int i = 0; i < 4; i++)
-          *(f32x4_t*)(r + pair * D + dt * 32 + i * 8 + half * 4) =
-              f32x4_t{o[n][dt][4 * i], o[n][dt][4 * i + 1], o[n][dt][4 * i + 2], o[n][dt][4 * i + 3]};
-      if (half == 0) *(float2*)(r + (int64_t)lay.rec_rows * D + 2 * pair) = make_float2(m_ref[n], sum);
-    }
+    for (int dt = 0; dt < DT; dt++)
+#pragma unroll
+      for (int i = 0; i < 4; i++)
+        *(f32x4_t*)(r + pair * D + dt * 32 + i * 8 + half * 4) =
+            f32x4_t{o[dt][4 * i], o[dt][4 * i + 1], o[dt][4 * i + 2], o[dt][4 * i + 3]};
+    if (half == 0) *(float2*)(r + (int64_t)lay.rec_rows * D + 2 * pair) = make_float2(m_ref, sum);
   }
 }
 
@@ -532,19 +575,16 @@ __global__ void __launch_bounds__(256) k_attn_rows_join(AttnRowsCall c, Layout l
   }
 }
 
-constexpr int kNR = 1;
-
 template <int D>
 hipError_t launch_d(const AttnRowsCall& c, hipStream_t s) {
-  constexpr int kTileRows = 32 * kNR * kWaves;
   const Layout lay = layout_of(c.batch, c.max_rows, c.hq, c.kv.hkv, D, c.max_seq, c.num_cus, kTileRows);
   k_attn_rows_plan<<<1, 1024, (size_t)(c.batch + 1) * sizeof(int32_t), s>>>(c, lay, kTileRows);
-  const size_t lds = 2 * (size_t)(kChunkBlocks * (kBlockTokens * D * 2 + 2 * (D * 16 + 128)));
-  if (lds > 64 * 1024) {
-    const hipError_t e = hipFuncSetAttribute((const void*)k_attn_rows<D, kNR>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+  const size_t lds = 2 * kRing * (size_t)kChunk * D * 2;
+  if (lds > 32 * 1024) {
+    const hipError_t e = hipFuncSetAttribute((const void*)k_attn_rows<D>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     if (e != hipSuccess) return e;
   }
-  k_attn_rows<D, kNR><<<(unsigned)((int64_t)lay.pairs_cap * c.kv.hkv), 256, lds, s>>>(c, lay);
+  k_attn_rows<D><<<(unsigned)((int64_t)lay.pairs_cap * c.kv.hkv), 256, lds, s>>>(c, lay);
   k_attn_rows_join<D><<<dim3(lay.cuts_cap, c.kv.hkv), 256, 0, s>>>(c, lay, kTileRows);
   return hipGetLastError();
 }
@@ -552,7 +592,7 @@ hipError_t launch_d(const AttnRowsCall& c, hipStream_t s) {
 }  // namespace
 
 size_t attn_rows_ws_bytes(int batch, int max_rows, int hq, int hkv, int d, int max_seq, int num_cus) {
-  return layout_of(batch, max_rows, hq, hkv, d, max_seq, num_cus, 32 * kNR * kWaves).bytes;
+  return layout_of(batch, max_rows, hq, hkv, d, max_seq, num_cus, kTileRows).bytes;
 }
 
 hipError_t launch_attention_rows(const AttnRowsCall& c, hipStream_t s) {
