@@ -290,49 +290,50 @@ __global__ void __launch_bounds__(256, 2) k_attn_rows(AttnRowsCall c, Layout lay
   const int wave_most = wave_live ? first_pos + min(tokens, (wave * 32 + 31) / group + 1) : 0;
 
   f32x16_t o[DT];
-  float m_ref = live ? -INFINITY : 0.f, l = 0.f;
+  // A score x weighs 2^(x scale + base). `most`: the largest sum of a chunk's weights that leaves base alone; negative before there
+  // is a reference, kMost from then on (and for lanes without a pair).
+  float base = 0.f, most = live ? -1.f : kMost, l = 0.f;
 #pragma unroll
   for (int dt = 0; dt < DT; dt++)
 #pragma unroll
     for (int r = 0; r < 16; r++) o[dt][r] = 0.f;
 
-  // Block ids of 32 chunks, one a lane, and of the 32 behind them (loaded a group
-  // ahead: a wait for an id would wait for the chunks in flight too). A block
-  // outside the cache is read as block 0, places past the last block as the last.
+  // Places in the cache (in blocks of one KV head) of 32 chunks' blocks, one a
+  // lane, and the ids of the 32 behind them (loaded a group ahead: a wait for an id
+  // would wait for the chunks in flight too). A block outside the cache is read as
+  // block 0, one past the last block as the last.
   bool bad = false;
   auto load_ids = [&](int chunk) { return bt[min(chunk * kChunkBlocks + lane, blocks - 1)]; };
-  auto checked = [&](int id) {
+  const int place0 = c.region * c.kv.nblk;
+  auto places = [&](int id) {
     const bool ok = id >= 0 && id < c.kv.nblk;
     bad |= !ok;
-    return ok ? id : 0;
+    return (place0 + (ok ? id : 0)) * hkv + g;
   };
-  int ids_k = checked(load_ids(c0)), ids_next = load_ids(c0 + kGroupChunks), ids_v = ids_k;  // V is fetched two chunks later
-  const int64_t region_blk = (int64_t)c.region * c.kv.nblk;
+  int at_k = places(load_ids(c0)), ids_next = load_ids(c0 + kGroupChunks), at_v = at_k;  // V is fetched two chunks later
   const int blk_wave = wave / kBlockWaves, in_block = wave % kBlockWaves;
   // K blocks go to LDS as they are; V blocks as [token / 8][d][token % 8], so that 32 dims' pieces are contiguous
   const uint32_t k_src = (in_block * 64 + lane) * 16;
   const uint32_t v_src = (in_block % (kBlockWaves / 2) * 64 + lane) * 32 + in_block / (kBlockWaves / 2) * 16;
-  auto fetch = [&](int ch, int ids, const void* cache, uint32_t src, char* ring) {
+  char* const mine = smem + blk_wave * kBlockBytes + in_block * 1024;  // this wave's first piece of a chunk
+  auto fetch = [&](int n, int at, const void* cache, uint32_t src, char* to) {  // n: chunk counted from c0
 #pragma unroll
     for (int j = 0; j < kPieces; j++) {
-      const int in_chunk = j * (kWaves / kBlockWaves) + blk_wave;
-      const int blk = __builtin_amdgcn_readlane(ids, (ch - c0) % kGroupChunks * kChunkBlocks + in_chunk);
-      load_lds16((const char*)cache + ((region_blk + blk) * hkv + g) * (int64_t)kBlockBytes + src,
-                 ring + (ch - c0) % kRing * kSide + in_chunk * kBlockBytes + in_block * 1024);
+      const int from = j * (kWaves / kBlockWaves);
+      const int place = __builtin_amdgcn_readlane(at, n % kGroupChunks * kChunkBlocks + from + blk_wave);
+      load_lds16((const char*)cache + (int64_t)place * kBlockBytes + src, to + from * kBlockBytes);
     }
   };
-  auto fetch_k = [&](int ch) {
-    if (ch >= c1) return;
-    if (ch > c0 && (ch - c0) % kGroupChunks == 0) {
-      ids_k = checked(ids_next);
-      ids_next = load_ids(ch + kGroupChunks);
+  auto fetch_k = [&](int n, int slot) {
+    if (n > 0 && n % kGroupChunks == 0) {
+      at_k = places(ids_next);
+      ids_next = load_ids(c0 + n + kGroupChunks);
     }
-    fetch(ch, ids_k, c.kv.k, k_src, smem);
+    fetch(n, at_k, c.kv.k, k_src, mine + slot * kSide);
   };
-  auto fetch_v = [&](int ch) {
-    if (ch >= c1) return;
-    if ((ch - c0) % kGroupChunks == 0) ids_v = ids_k;
-    fetch(ch, ids_v, c.kv.v, v_src, smem + kRing * kSide);
+  auto fetch_v = [&](int n, int slot) {
+    if (n % kGroupChunks == 0) at_v = at_k;
+    fetch(n, at_v, c.kv.v, v_src, mine + (kRing + slot) * kSide);
   };
   // Waits until this wave's loads but the last 4 * kPieces have landed (all, with `all`), then for the other waves.
   auto landed = [&](bool all) {
@@ -375,14 +376,6 @@ __global__ void __launch_bounds__(256, 2) k_attn_rows(AttnRowsCall c, Layout lay
   const int ktok = (col & 3) | ((col >> 2) & 1) << 3 | ((col >> 3) & 1) << 2;
   const uint32_t k_lane = (col >> 4) * kBlockBytes + (half * 16 + ktok) * 16;
   const uint32_t v_lane = half * (D * 16) + col * 16;
-  auto scores = [&](int ch, f32x16_t& s) {
-    const char* kb = smem + (ch - c0) % kRing * kSide + k_lane;
-#pragma unroll
-    for (int r = 0; r < 16; r++) s[r] = 0.f;
-#pragma unroll
-    for (int kk = 0; kk < KK; kk++)
-      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(*(const u32x4_t*)(kb + kk * 512)), q[kk], s, 0, 0, 0);
-  };
   // Register r: token 16 (r / 8) + 8 half + r % 8 of the chunk.
   auto mask = [&](int ch, f32x16_t& s) {
     if ((ch + 1) * kChunk > wave_least) {
@@ -390,42 +383,41 @@ __global__ void __launch_bounds__(256, 2) k_attn_rows(AttnRowsCall c, Layout lay
       for (int r = 0; r < 16; r++) s[r] = ch * kChunk + 16 * (r / 8) + 8 * half + r % 8 < limit ? s[r] : -INFINITY;
     }
   };
-  // The weights of a chunk's keys against the reference as it is, and their sum.
-  auto weights = [&](const f32x16_t& s, bf16x8_t (&p)[2]) {
-    const float base = m_ref == -INFINITY ? 0.f : -m_ref;
-    float sum = 0.f;
-#pragma unroll
-    for (int k = 0; k < 2; k++) {
-      float e[8];
-#pragma unroll
-      for (int r = 0; r < 8; r++) {
-        e[r] = __builtin_amdgcn_exp2f(fmaf(s[8 * k + r], scale, base));
-        sum += e[r];
-      }
-      p[k] = as_bf16x8(u32x4_t{pack_bf2(e[0], e[1]), pack_bf2(e[2], e[3]), pack_bf2(e[4], e[5]), pack_bf2(e[6], e[7])});
-    }
-    return sum;
-  };
-  // Moves the reference to the chunk's largest score where the weights have grown too large for the one they had.
+  // Where a pair's weights of a chunk have grown too large for its reference (or it has none): the reference moves to the chunk's
+  // largest score, the sums with it, and the weights are made again.
   auto weigh = [&](const f32x16_t& s, bf16x8_t (&p)[2], float sum) {
-    if (__any(sum > kMost || m_ref == -INFINITY)) {
+    if (__any(sum > most)) {
       float cm = s[0];
 #pragma unroll
       for (int r = 1; r < 16; r++) cm = fmaxf(cm, s[r]);
-      const float m_new = fmaxf(m_ref, max_halves(cm) * scale);
-      const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_ref - m_new);
-      m_ref = m_new;
-      l *= alpha;
+      cm = max_halves(cm) * scale;
+      const float old = most < 0.f ? -INFINITY : -base, now = fmaxf(old, cm);
+      if (now > -INFINITY) {
+        const float alpha = __builtin_amdgcn_exp2f(old - now);
+        base = -now;
+        most = kMost;
+        l *= alpha;
 #pragma unroll
-      for (int dt = 0; dt < DT; dt++)
+        for (int dt = 0; dt < DT; dt++)
 #pragma unroll
-        for (int r = 0; r < 16; r++) o[dt][r] *= alpha;
-      sum = weights(s, p);
+          for (int r = 0; r < 16; r++) o[dt][r] *= alpha;
+      }
+      sum = 0.f;
+#pragma unroll
+      for (int k = 0; k < 2; k++) {
+        float e[8];
+#pragma unroll
+        for (int r = 0; r < 8; r++) {
+          e[r] = __builtin_amdgcn_exp2f(fmaf(s[8 * k + r], scale, base));
+          sum += e[r];
+        }
+        p[k] = as_bf16x8(u32x4_t{pack_bf2(e[0], e[1]), pack_bf2(e[2], e[3]), pack_bf2(e[4], e[5]), pack_bf2(e[6], e[7])});
+      }
     }
     l += sum;
   };
-  auto add_values = [&](int ch, const bf16x8_t (&p)[2]) {
-    const char* vb = smem + (kRing + (ch - c0) % kRing) * kSide + v_lane;
+  auto add_values = [&](int slot, const bf16x8_t (&p)[2]) {
+    const char* vb = smem + (kRing + slot) * kSide + v_lane;
 #pragma unroll
     for (int k = 0; k < 2; k++)
 #pragma unroll
@@ -433,77 +425,108 @@ __global__ void __launch_bounds__(256, 2) k_attn_rows(AttnRowsCall c, Layout lay
         o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(*(const u32x4_t*)(vb + k * kBlockBytes + dt * 512)), p[k], o[dt],
                                                         0, 0, 0);
   };
-  // A turn makes chunk ch's weights on the vector units while the matrix units add chunk ch - 1's values and make chunk ch + 1's
-  // scores: at its start V(ch - 1) and K(ch + 1) have landed, and V(ch + 2) and K(ch + 4) are fetched into the places of V(ch - 2)
-  // and K(ch), three turns before their use. (Behind the last chunk the scores are of whatever lies there, and nobody's.)
-  auto turn = [&](auto first, int ch, f32x16_t& s, f32x16_t& s_next, bf16x8_t (&p_last)[2], bf16x8_t (&p)[2]) {
+  // Chunk ch's weights on the vector units, while the matrix units add chunk ch - 1's values (not with `first`) and make chunk
+  // ch + 1's scores. Products take turns between the two, each with its share of the weights' arithmetic behind it, and fragments
+  // are read kAhead products ahead. (Behind the last chunk the scores are of whatever lies there, and nobody's.)
+  auto products = [&](auto first, int slot, f32x16_t& s, f32x16_t& s_next, bf16x8_t (&p_last)[2], bf16x8_t (&p)[2]) {
     constexpr bool kFirst = decltype(first)::value;
-    fetch_v(ch + 2);
-    fetch_k(ch + 4);
-    if (ch * kChunk < wave_most) {
-      mask(ch, s);
-      // Products take turns between the two, each with its share of the weights' arithmetic behind it, and fragments are read
-      // kAhead products ahead.
-      constexpr int kProducts = KK + (kFirst ? 0 : 2 * DT), kShare = 16 / kProducts, kAhead = 3;
-      const char* kb = smem + (ch + 1 - c0) % kRing * kSide + k_lane;
-      const char* vb = smem + (kRing + (ch + kRing - 1 - c0) % kRing) * kSide + v_lane;
-      u32x4_t frag[kAhead + 1];
-      auto read = [&](int i) {
-        const char* from = kFirst ? kb + i * 512 : i % 2 ? kb + i / 2 * 512 : vb + i / 2 / DT * kBlockBytes + i / 2 % DT * 512;
-        frag[i % (kAhead + 1)] = *(const u32x4_t*)from;
-      };
-      const float base = m_ref == -INFINITY ? 0.f : -m_ref;
-      float sum = 0.f, e[16];
+    constexpr int kProducts = KK + (kFirst ? 0 : 2 * DT), kShare = 16 / kProducts, kAhead = 3;
+    const char* kb = smem + (slot + 1) % kRing * kSide + k_lane;
+    const char* vb = smem + (kRing + (slot + kRing - 1) % kRing) * kSide + v_lane;
+    u32x4_t frag[kAhead + 1];
+    auto read = [&](int i) {
+      const char* from = kFirst ? kb + i * 512 : i % 2 ? kb + i / 2 * 512 : vb + i / 2 / DT * kBlockBytes + i / 2 % DT * 512;
+      frag[i % (kAhead + 1)] = *(const u32x4_t*)from;
+    };
+    float sum = 0.f, e[16];
 #pragma unroll
-      for (int r = 0; r < 16; r++) s_next[r] = 0.f;
+    for (int r = 0; r < 16; r++) s_next[r] = 0.f;
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int i = 0; i < kAhead; i++) read(i);
+    for (int i = 0; i < kAhead; i++) read(i);
 #pragma unroll
-      for (int i = 0; i < kProducts; i++) {
-        __builtin_amdgcn_sched_barrier(0);
-        if (i + kAhead < kProducts) read(i + kAhead);
-        const bf16x8_t f = as_bf16x8(frag[i % (kAhead + 1)]);
-        if (kFirst || i % 2) s_next = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, q[kFirst ? i : i / 2], s_next, 0, 0, 0);
-        else o[i / 2 % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, p_last[i / 2 / DT], o[i / 2 % DT], 0, 0, 0);
+    for (int i = 0; i < kProducts; i++) {
+      __builtin_amdgcn_sched_barrier(0);
+      if (i + kAhead < kProducts) read(i + kAhead);
+      const bf16x8_t f = as_bf16x8(frag[i % (kAhead + 1)]);
+      if (kFirst || i % 2) s_next = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, q[kFirst ? i : i / 2], s_next, 0, 0, 0);
+      else o[i / 2 % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, p_last[i / 2 / DT], o[i / 2 % DT], 0, 0, 0);
 #pragma unroll
-        for (int r = i * kShare; r < (i + 1) * kShare; r++) {
-          e[r] = __builtin_amdgcn_exp2f(fmaf(s[r], scale, base));
-          if (r > 0) sum += e[r - 1];  // a step late: nothing waits for the exponential
-          if (r % 8 == 7) {
-            const float* w = e + r - 7;
-            p[r / 8] = as_bf16x8(u32x4_t{pack_bf2(w[0], w[1]), pack_bf2(w[2], w[3]), pack_bf2(w[4], w[5]), pack_bf2(w[6], w[7])});
-          }
+      for (int r = i * kShare; r < (i + 1) * kShare; r++) {
+        e[r] = __builtin_amdgcn_exp2f(fmaf(s[r], scale, base));
+        if (r > 0) sum += e[r - 1];  // a step late: nothing waits for the exponential
+        if (r % 8 == 7) {
+          const float* w = e + r - 7;
+          p[r / 8] = as_bf16x8(u32x4_t{pack_bf2(w[0], w[1]), pack_bf2(w[2], w[3]), pack_bf2(w[4], w[5]), pack_bf2(w[6], w[7])});
         }
       }
-      __builtin_amdgcn_sched_barrier(0);
-      sum += e[15];
-      weigh(s, p, sum);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    weigh(s, p, sum + e[15]);
+  };
+  // A turn for chunk c0 + n: at its start V(n - 1) and K(n + 1) have landed, and V(n + 2) and K(n + 4) are fetched into the places
+  // of V(n - 2) and K(n), three turns before their use.
+  auto turn = [&](auto first, int n, f32x16_t& s, f32x16_t& s_next, bf16x8_t (&p_last)[2], bf16x8_t (&p)[2]) {
+    constexpr bool kFirst = decltype(first)::value;
+    const int ch = c0 + n, slot = n % kRing;
+    if (ch + 2 < c1) fetch_v(n + 2, (n + 2) % kRing);
+    if (ch + 4 < c1) fetch_k(n + 4, slot);
+    if (ch * kChunk < wave_most) {
+      mask(ch, s);
+      products(first, slot, s, s_next, p_last, p);
     } else if (!kFirst && (ch - 1) * kChunk < wave_most) {
-      add_values(ch - 1, p_last);
+      add_values((n + kRing - 1) % kRing, p_last);
     }
     landed(ch + 4 >= c1);
     mend(ch);
   };
   f32x16_t sa, sb;
   bf16x8_t pa[2], pb[2];
-  fetch_k(c0);
-  fetch_k(c0 + 1);
-  fetch_v(c0);
-  fetch_k(c0 + 2);
-  fetch_v(c0 + 1);
-  fetch_k(c0 + 3);
-  landed(c0 + 4 > c1);
-  if (c0 * kChunk < wave_most) scores(c0, sa);
-  __builtin_amdgcn_s_barrier();  // K(c0) is read
+  const int n_end = c1 - c0;
+  fetch_k(0, 0);
+  if (1 < n_end) fetch_k(1, 1);
+  fetch_v(0, 0);
+  if (2 < n_end) fetch_k(2, 2);
+  if (1 < n_end) fetch_v(1, 1);
+  if (3 < n_end) fetch_k(3, 3);
+  landed(4 > n_end);
+  if (c0 * kChunk < wave_most) {
+    const char* kb = smem + k_lane;
+#pragma unroll
+    for (int r = 0; r < 16; r++) sa[r] = 0.f;
+#pragma unroll
+    for (int kk = 0; kk < KK; kk++) sa = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(*(const u32x4_t*)(kb + kk * 512)), q[kk], sa, 0, 0, 0);
+  }
+  __builtin_amdgcn_s_barrier();  // K(0) is read
   asm volatile("" ::: "memory");
-  turn(std::true_type{}, c0, sa, sb, pb, pa);
-  for (int ch = c0 + 1; ch < c1; ch += 2) {
-    turn(std::false_type{}, ch, sb, sa, pa, pb);
-    if (ch + 1 < c1) turn(std::false_type{}, ch + 1, sa, sb, pb, pa);
+  turn(std::true_type{}, 0, sa, sb, pb, pa);
+  int n = 1;
+  {
+    // Turns that every row of the tile sees whole and that have chunks to fetch: the same without the questions, four at a time
+    // so that their places in the rings are constants.
+    auto plain = [&](auto slot, f32x16_t& s, f32x16_t& s_next, bf16x8_t (&p_last)[2], bf16x8_t (&p)[2]) {
+      constexpr int kSlot = decltype(slot)::value;
+      fetch_v(n + 2, (kSlot + 2) % kRing);
+      fetch_k(n + 4, kSlot);
+      if (wave_live) products(std::false_type{}, kSlot, s, s_next, p_last, p);
+      landed(false);
+      n++;
+    };
+    const int plain_end = min(n_end - 4, (first_pos + 1) / kChunk - c0);
+    while (n + 3 < plain_end) {
+      plain(std::integral_constant<int, 1>{}, sb, sa, pa, pb);
+      plain(std::integral_constant<int, 2>{}, sa, sb, pb, pa);
+      plain(std::integral_constant<int, 3>{}, sb, sa, pa, pb);
+      plain(std::integral_constant<int, 0>{}, sa, sb, pb, pa);
+    }
+  }
+  for (; n < n_end; n += 2) {
+    turn(std::false_type{}, n, sb, sa, pa, pb);
+    if (n + 1 < n_end) turn(std::false_type{}, n + 1, sa, sb, pb, pa);
   }
   if ((c1 - 1) * kChunk < wave_most) {
-    if ((c1 - c0) & 1) add_values(c1 - 1, pa);
-    else add_values(c1 - 1, pb);
+    if (n_end & 1) add_values((n_end - 1) % kRing, pa);
+    else add_values((n_end - 1) % kRing, pb);
   }
   if (bad) atomicOr(c.err, SIDP_DEVERR_BLOCK);
 
@@ -539,7 +562,7 @@ __global__ void __launch_bounds__(256, 2) k_attn_rows(AttnRowsCall c, Layout lay
       for (int i = 0; i < 4; i++)
         *(f32x4_t*)(r + pair * D + dt * 32 + i * 8 + half * 4) =
             f32x4_t{o[dt][4 * i], o[dt][4 * i + 1], o[dt][4 * i + 2], o[dt][4 * i + 3]};
-    if (half == 0) *(float2*)(r + (int64_t)lay.rec_rows * D + 2 * pair) = make_float2(m_ref, sum);
+    if (half == 0) *(float2*)(r + (int64_t)lay.rec_rows * D + 2 * pair) = make_float2(most < 0.f ? -INFINITY : -base, sum);
   }
 }
 
