@@ -45,8 +45,8 @@ typedef const __attribute__((address_space(4))) int32_t cint32_t;
 
 struct Entry {
   int b, tile;
-  int run;  // first chunk | chunks << 16
-  int rec;  // record of a cut tile, -1 for a whole one
+  uint32_t run;  // first chunk | chunks << 16, at most 2^15
+  int rec;        // record of a cut tile, -1 for a whole one
 };
 struct Cut {
   int b, tile, parts, rec;
@@ -54,22 +54,23 @@ struct Cut {
 
 // Workspace: counts, entries, cut tiles, records (o [rows][D], then m and l of each row).
 struct Layout {
-  int pairs_cap;                     // entries
-  int cuts_cap, recs_cap, rec_rows;  // cut tiles, records, rows of a record
+  int tiles_cap, entries_cap;
+  int cuts_cap, recs_cap, rec_rows;  // cut tiles, records, pairs of a record
   size_t entries, cuts, recs, bytes;
 };
 
-__host__ __device__ inline int tile_tokens(int group, int tile_rows) { return tile_rows / group; }
+__host__ __device__ inline int tile_tokens(int group) { return kTileRows / group; }
+__host__ __device__ inline int slots_of(int num_cus, int hkv) { return kSlotsPerCu * (num_cus < 1 ? 1 : num_cus) / hkv; }  // for one KV head's items
 
-Layout layout_of(int batch, int max_rows, int hq, int hkv, int d, int max_seq, int num_cus, int tile_rows) {
-  const int group = hq / hkv, tm = tile_tokens(group, tile_rows), slots = kSlotsPerCu * std::max(1, num_cus);
+Layout layout_of(int batch, int max_rows, int hq, int hkv, int d, int max_seq, int num_cus) {
+  const int group = hq / hkv, tm = tile_tokens(group), slots = slots_of(num_cus, hkv);
   Layout l;
-  const int tiles = (int)std::min<int64_t>(max_rows, (int64_t)max_rows / tm + std::min(batch, max_rows));
+  l.tiles_cap = (int)std::min<int64_t>(max_rows, (int64_t)max_rows / tm + std::min(batch, max_rows));
+  l.cuts_cap = std::min(l.tiles_cap, std::max(slots - 1, 0));  // a call with more tiles is not cut
+  // a run is at least kMinRun chunks, and the total over slots: at most slots runs more than tiles
   const int runs = (max_seq + kChunk * kMinRun - 1) / (kChunk * kMinRun);
-  l.cuts_cap = std::min(tiles, slots / hkv + 1);
-  // a run is at least total / slots chunks: at most slots runs more than tiles
-  l.recs_cap = (int)std::min<int64_t>((int64_t)l.cuts_cap * runs, l.cuts_cap + slots / hkv + 1);
-  l.pairs_cap = std::max(tiles, l.recs_cap);
+  l.recs_cap = (int)std::min<int64_t>((int64_t)l.cuts_cap * runs, l.cuts_cap + slots);
+  l.entries_cap = std::max(l.tiles_cap, l.recs_cap);
   l.rec_rows = std::min(tm, max_rows) * group;
   size_t o = 64;
   auto place = [&](size_t n) {
@@ -77,85 +78,147 @@ Layout layout_of(int batch, int max_rows, int hq, int hkv, int d, int max_seq, i
     o = (o + n + 255) / 256 * 256;
     return at;
   };
-  l.entries = place((size_t)l.pairs_cap * sizeof(Entry));
+  l.entries = place((size_t)l.entries_cap * sizeof(Entry));
   l.cuts = place((size_t)l.cuts_cap * sizeof(Cut));
   l.recs = place((size_t)l.recs_cap * hkv * l.rec_rows * (d + 2) * sizeof(float));
   l.bytes = o;
   return l;
 }
 
-// Lists the tiles, longest run first, so that the launch ends evenly.
-__global__ void __launch_bounds__(1024) k_attn_rows_plan(AttnRowsCall c, Layout lay, int tile_rows) {
-  extern __shared__ int32_t s_first[];  // [batch + 1] first tile of each sequence
-  __shared__ int s_scan[16], s_longest[16];
-  __shared__ long long s_total[16];
+// Lists the items. One workgroup, a chain of latencies in front of the attention:
+// lengths are read once, into LDS, and only as many waves work as there are
+// sequences or tiles (16 sequences of 4 rows: 4 us; 9 with 16 waves).
+//
+// At least as many tiles as the chip holds at once: longest first, so that the
+// launch ends evenly. Fewer: every tile is cut into even runs of at most `run`
+// chunks, the shortest of kTries lengths between an even share of all chunks and one
+// that cannot give more runs than fit (a tile's last run may be short: half a run
+// a tile lies between the two).
+constexpr int kTries = 8;
+constexpr int kPlanWaves = 16;
+__global__ void __launch_bounds__(64 * kPlanWaves) k_attn_rows_plan(AttnRowsCall c, Layout lay) {
+  extern __shared__ int32_t s_lds[];
+  int32_t* s_first = s_lds;                // [batch + 1] first tile of each sequence
+  int32_t* s_ctx = s_first + c.batch + 1;  // [batch] cached tokens
+  int32_t* s_rows = s_ctx + c.batch;       // [batch] rows
+  __shared__ int s_scan[kPlanWaves], s_longest[kPlanWaves], s_parts[kPlanWaves];
+  __shared__ uint32_t s_total[kPlanWaves];
   __shared__ int s_hist[256];
-  __shared__ int s_cuts, s_recs;
-  const int t = threadIdx.x, wave = t >> 6, lane = t & 63;
-  const int group = c.hq / c.kv.hkv, tm = tile_tokens(group, tile_rows);
-  const int slots = kSlotsPerCu * max(1, c.num_cus);
+  __shared__ int s_items[kTries];
+  __shared__ int s_base[64 * kPlanWaves];
+  __shared__ int s_cuts;
+  const int t = threadIdx.x, wave = t >> 6, lane = t & 63, threads = blockDim.x, waves = threads / 64;
+  const int group = c.hq / c.kv.hkv, tm = tile_tokens(group);
+  const int slots = slots_of(c.num_cus, c.kv.hkv);
   char* ws = (char*)c.ws;
   int32_t* counts = (int32_t*)ws;
   Entry* entries = (Entry*)(ws + lay.entries);
-  Cut* cuts = (Cut*)(ws + lay.cuts);
-  // rows of a sequence; none (and an error) for starts or lengths that the call does not cover
-  uint32_t bad = 0;
-  auto rows_of = [&](int b) {
+  if (t < kTries) s_items[t] = 0;
+  if (t == 0) s_cuts = 0;
+  // a sequence whose starts or lengths the call does not cover has no rows
+  bool bad = false;
+  for (int b = t; b < c.batch; b += threads) {
     const int r0 = c.row_starts[b], r1 = c.row_starts[b + 1], ctx = c.ctx_lens[b];
-    if (r0 < 0 || r1 < r0 || r1 > c.max_rows || ctx < 0 || (int64_t)ctx + (r1 - r0) > (int64_t)c.max_blocks * kBlockTokens ||
-        (int64_t)ctx + (r1 - r0) > c.max_seq) {
-      bad = SIDP_DEVERR_POSITION;
-      return 0;
-    }
-    return r1 - r0;
-  };
-  const int per = (c.batch + 1023) / 1024;
-  const int b0 = min(t * per, c.batch), b1 = min(b0 + per, c.batch);
-  int mine = 0;
-  for (int b = b0; b < b1; b++) mine += (rows_of(b) + tm - 1) / tm;
-  int incl = mine;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int v = __shfl_up(incl, o, 64);
-    if (lane >= o) incl += v;
+    const bool ok = r0 >= 0 && r1 >= r0 && r1 <= c.max_rows && ctx >= 0 &&
+                    (int64_t)ctx + (r1 - r0) <= (int64_t)min(c.max_blocks * kBlockTokens, c.max_seq);
+    bad |= !ok;
+    s_ctx[b] = ctx;
+    s_rows[b] = ok ? r1 - r0 : 0;
   }
-  if (lane == 63) s_scan[wave] = incl;
-  if (t < 256) s_hist[t] = 0;
-  if (t == 0) s_cuts = s_recs = 0;
+  if (bad) atomicOr(c.err, SIDP_DEVERR_POSITION);
   __syncthreads();
-  int at = incl - mine;
-  for (int w = 0; w < wave; w++) at += s_scan[w];
+  // exclusive place of a thread's `mine` among all threads', and the sum
+  auto scan = [&](int mine, int* s_sums, int& sum) {
+    int incl = mine;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int v = __shfl_up(incl, o, 64);
+      if (lane >= o) incl += v;
+    }
+    if (lane == 63) s_sums[wave] = incl;
+    __syncthreads();
+    int at = incl - mine;
+    sum = 0;
+    for (int w = 0; w < waves; w++) {
+      if (w < wave) at += s_sums[w];
+      sum += s_sums[w];
+    }
+    return at;
+  };
+  const int per = (c.batch + threads - 1) / threads;
+  const int b0 = min(t * per, c.batch), b1 = min(b0 + per, c.batch);
+  int mine = 0, tiles;
+  for (int b = b0; b < b1; b++) mine += (s_rows[b] + tm - 1) / tm;
+  int at = scan(mine, s_scan, tiles);
   for (int b = b0; b < b1; b++) {
     s_first[b] = at;
-    at += (rows_of(b) + tm - 1) / tm;
+    at += (s_rows[b] + tm - 1) / tm;
   }
-  int tiles = 0;
-  for (int w = 0; w < 16; w++) tiles += s_scan[w];
   if (t == 0) s_first[c.batch] = tiles;
-  if (bad) atomicOr(c.err, bad);
   __syncthreads();
-  // tile i: its sequence, place in it and chunks
-  auto tile_of = [&](int i, int& b, int& tile) {
-    int lo = 0, hi = c.batch;
+  tiles = min(tiles, lay.tiles_cap);  // row starts that overlap could list more
+  auto last_at = [](const int* s, int n, int i) {  // the last of s[0 .. n) that is at most i
+    int lo = 0, hi = n;
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
-      if (s_first[mid] <= i) lo = mid;
+      if (s[mid] <= i) lo = mid;
       else hi = mid;
     }
-    b = lo;
-    tile = i - s_first[lo];
-    const int n = c.row_starts[b + 1] - c.row_starts[b];
-    return (c.ctx_lens[b] + min(n, (tile + 1) * tm) + kChunk - 1) / kChunk;
+    return lo;
   };
-  tiles = min(tiles, lay.pairs_cap);  // row starts that overlap could list more
-  long long total = 0;
-  int longest = 0;
-  for (int i = t; i < tiles; i += 1024) {
-    int b, tile;
-    const int n = tile_of(i, b, tile);
-    total += n;
-    longest = max(longest, n);
+  // tile i: its sequence, place in it and chunks
+  struct Tile {
+    int b, place, chunks;
+  };
+  auto tile_of = [&](int i) {
+    const int b = last_at(s_first, c.batch, i), place = i - s_first[b];
+    return Tile{b, place, (s_ctx[b] + min(s_rows[b], (place + 1) * tm) + kChunk - 1) / kChunk};
+  };
+  if (tiles >= slots || tiles > lay.cuts_cap || tiles > threads) {
+    // a counting sort by length, in 256 steps of the longest one's
+    for (int i = t; i < 256; i += threads) s_hist[i] = 0;
+    int longest = 1;
+    for (int i = t; i < tiles; i += threads) longest = max(longest, tile_of(i).chunks);
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) longest = max(longest, __shfl_xor(longest, o, 64));
+    if (lane == 0) s_longest[wave] = longest;
+    __syncthreads();
+    for (int w = 0; w < waves; w++) longest = max(longest, s_longest[w]);
+    auto bucket = [&](int n) { return 255 - n * 255 / longest; };
+    for (int i = t; i < tiles; i += threads) atomicAdd(&s_hist[bucket(tile_of(i).chunks)], 1);
+    __syncthreads();
+    if (t < 64) {
+      int h[4], sum = 0;
+#pragma unroll
+      for (int j = 0; j < 4; j++) {
+        h[j] = sum;
+        sum += s_hist[4 * t + j];
+      }
+      int inc = sum;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const int v = __shfl_up(inc, o, 64);
+        if (lane >= o) inc += v;
+      }
+#pragma unroll
+      for (int j = 0; j < 4; j++) s_hist[4 * t + j] = inc - sum + h[j];
+    }
+    __syncthreads();
+    // Within a step the order is whatever the atomics give; items write places of their own, so results do not depend on it.
+    for (int i = t; i < tiles; i += threads) {
+      const Tile x = tile_of(i);
+      entries[atomicAdd(&s_hist[bucket(x.chunks)], 1)] = Entry{x.b, x.place, (uint32_t)x.chunks << 16, -1};
+    }
+    if (t == 0) {
+      counts[0] = tiles;
+      counts[1] = 0;
+    }
+    return;
   }
+  // a tile a thread at most
+  const Tile own = t < tiles ? tile_of(t) : Tile{0, 0, 0};
+  uint32_t total = own.chunks;
+  int longest = own.chunks;
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) {
     total += __shfl_xor(total, o, 64);
@@ -167,58 +230,46 @@ __global__ void __launch_bounds__(1024) k_attn_rows_plan(AttnRowsCall c, Layout 
   }
   __syncthreads();
   total = 0;
-  for (int w = 0; w < 16; w++) {
+  for (int w = 0; w < waves; w++) {
     total += s_total[w];
     longest = max(longest, s_longest[w]);
   }
-  // fewer items than slots: runs of an even share, at least kMinRun chunks
   int run = max(longest, 1);
-  if ((int64_t)tiles * c.kv.hkv < slots && tiles <= lay.cuts_cap) {
-    const int share = (int)((total * c.kv.hkv + slots - 1) / slots);
-    run = min(run, max(share, kMinRun));
-  }
-  auto bucket = [&](int n) { return 255 - (int)((int64_t)n * 255 / run); };
-  for (int i = t; i < tiles; i += 1024) {
-    int b, tile;
-    const int n = tile_of(i, b, tile);
-    if (n / run) atomicAdd(&s_hist[bucket(run)], n / run);
-    if (n % run) atomicAdd(&s_hist[bucket(n % run)], 1);
-  }
-  __syncthreads();
-  if (t < 64) {
-    // exclusive prefix of the 256 buckets, four a lane
-    int h[4], sum = 0;
-    for (int j = 0; j < 4; j++) {
-      h[j] = sum;
-      sum += s_hist[4 * t + j];
-    }
-    int inc = sum;
+  const int least = max((int)(total + slots - 1) / slots, kMinRun);
+  if (least < longest) {
+    const int most = max((int)(total + slots - tiles - 1) / (slots - tiles), least);
+    auto try_of = [&](int j) { return least + (most - least) * j / (kTries - 1); };
+    int n[kTries];
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int v = __shfl_up(inc, o, 64);
-      if (lane >= o) inc += v;
-    }
-    for (int j = 0; j < 4; j++) s_hist[4 * t + j] = inc - sum + h[j];
-    if (t == 63) counts[0] = inc;
+    for (int j = 0; j < kTries; j++) n[j] = (own.chunks + try_of(j) - 1) / try_of(j);
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1)
+#pragma unroll
+      for (int j = 0; j < kTries; j++) n[j] += __shfl_xor(n[j], o, 64);
+    if (lane == 0)
+#pragma unroll
+      for (int j = 0; j < kTries; j++) atomicAdd(&s_items[j], n[j]);
+    __syncthreads();
+    int j = 0;
+    while (j < kTries - 1 && s_items[j] > slots) j++;
+    run = min(run, try_of(j));
   }
+  int runs;
+  const int parts = (own.chunks + run - 1) / run, base = scan(parts, s_parts, runs);
+  s_base[t] = base;
+  if (parts > 1) ((Cut*)(ws + lay.cuts))[atomicAdd(&s_cuts, 1)] = Cut{own.b, own.place, parts, base};
   __syncthreads();
-  // Within a bucket the order is whatever the atomics give; entries write places of their own, so results do not depend on it.
-  for (int i = t; i < tiles; i += 1024) {
-    int b, tile;
-    const int n = tile_of(i, b, tile);
-    const int parts = (n + run - 1) / run;
-    int rec = -1;
-    if (parts > 1) {
-      rec = atomicAdd(&s_recs, parts);
-      cuts[atomicAdd(&s_cuts, 1)] = Cut{b, tile, parts, rec};
-    }
-    for (int p = 0; p < parts; p++) {
-      const int len = min(run, n - p * run);
-      entries[atomicAdd(&s_hist[bucket(len)], 1)] = Entry{b, tile, p * run | len << 16, parts > 1 ? rec + p : -1};
-    }
+  for (int e = t; e < runs; e += threads) {
+    const int i = last_at(s_base, tiles, e);
+    const Tile x = tile_of(i);
+    const int p = e - s_base[i], n = (x.chunks + run - 1) / run;
+    const int lo = x.chunks * p / n, hi = x.chunks * (p + 1) / n;
+    entries[e] = Entry{x.b, x.place, (uint32_t)lo | (uint32_t)(hi - lo) << 16, n > 1 ? e : -1};
   }
-  __syncthreads();
-  if (t == 0) counts[1] = s_cuts;
+  if (t == 0) {
+    counts[0] = runs;
+    counts[1] = s_cuts;
+  }
 }
 
 __device__ __forceinline__ uint32_t keep_finite(uint32_t v) {
@@ -256,12 +307,12 @@ __global__ void __launch_bounds__(256, 2) k_attn_rows(AttnRowsCall c, Layout lay
   const int t = threadIdx.x, lane = t & 63, col = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const char* ws = (const char*)c.ws;
-  const int hkv = c.kv.hkv, group = c.hq / hkv, tm = tile_tokens(group, kTileRows);
+  const int hkv = c.kv.hkv, group = c.hq / hkv, tm = tile_tokens(group);
   const int item = blockIdx.x;
   if (item >= ((cint32_t*)ws)[0] * hkv) return;
   cint32_t* ep = (cint32_t*)(ws + lay.entries) + (item / hkv) * 4;
   const int g = item % hkv;
-  const int b = ep[0], tile = ep[1], c0 = ep[2] & 0xffff, c1 = c0 + (ep[2] >> 16), rec = ep[3];
+  const int b = ep[0], tile = ep[1], c0 = ep[2] & 0xffff, c1 = c0 + (int)((uint32_t)ep[2] >> 16), rec = ep[3];
   const int row0 = ((cint32_t*)c.row_starts)[b] + tile * tm;
   const int tokens = min(tm, ((cint32_t*)c.row_starts)[b + 1] - row0);  // of this tile
   const int first_pos = ((cint32_t*)c.ctx_lens)[b] + tile * tm;         // of its first row
@@ -566,56 +617,77 @@ __global__ void __launch_bounds__(256, 2) k_attn_rows(AttnRowsCall c, Layout lay
   }
 }
 
-// Joins a cut tile's records in run order: one workgroup per (cut tile, KV head), four dims a thread.
+// Joins a cut tile's records in run order: four dims a thread, 1024 / D pairs of one (cut tile, KV head) a workgroup, the records
+// of kJoin runs in flight at a time.
+constexpr int kJoin = 8;
 template <int D>
-__global__ void __launch_bounds__(256) k_attn_rows_join(AttnRowsCall c, Layout lay, int tile_rows) {
+__global__ void __launch_bounds__(256) k_attn_rows_join(AttnRowsCall c, Layout lay) {
   const char* ws = (const char*)c.ws;
   if ((int)blockIdx.x >= ((const int32_t*)ws)[1]) return;
   const Cut cut = ((const Cut*)(ws + lay.cuts))[blockIdx.x];
-  const int hkv = c.kv.hkv, g = blockIdx.y, group = c.hq / hkv, tm = tile_tokens(group, tile_rows);
+  const int hkv = c.kv.hkv, g = blockIdx.y, group = c.hq / hkv, tm = tile_tokens(group);
   const int row0 = c.row_starts[cut.b] + cut.tile * tm;
   const int pairs = min(tm, c.row_starts[cut.b + 1] - row0) * group;
+  const int pair = blockIdx.z * (1024 / D) + threadIdx.x / (D / 4), d = threadIdx.x % (D / 4) * 4;
+  if (pair >= pairs) return;
   const int64_t step = (int64_t)hkv * lay.rec_rows * (D + 2);
-  const float* recs = (const float*)(ws + lay.recs) + ((int64_t)cut.rec * hkv + g) * lay.rec_rows * (D + 2);
-  const float* ml = recs + (int64_t)lay.rec_rows * D;
-  for (int i = threadIdx.x; i < pairs * (D / 4); i += 256) {
-    const int pair = i / (D / 4), d = i % (D / 4) * 4;
-    float M = -INFINITY;
-    for (int p = 0; p < cut.parts; p++) M = fmaxf(M, ml[p * step + 2 * pair]);
-    float L = 0.f;
-    f32x4_t O = {0.f, 0.f, 0.f, 0.f};
-    for (int p = 0; p < cut.parts; p++) {
-      const float m = ml[p * step + 2 * pair];
-      const f32x4_t v = *(const f32x4_t*)(recs + p * step + (int64_t)pair * D + d);
-      // a run of which the pair sees nothing left zeros
-      const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - M);
-      L = fmaf(ml[p * step + 2 * pair + 1], f, L);
-      O += v * f;
+  const float* rec = (const float*)(ws + lay.recs) + ((int64_t)cut.rec * hkv + g) * lay.rec_rows * (D + 2);
+  const float* ml = rec + (int64_t)lay.rec_rows * D + 2 * pair;
+  rec += (int64_t)pair * D + d;
+  float M = -INFINITY, L = 0.f;
+  f32x4_t O = {0.f, 0.f, 0.f, 0.f};
+  for (int p0 = 0; p0 < cut.parts; p0 += kJoin) {
+    float2 r[kJoin];
+    f32x4_t v[kJoin];
+#pragma unroll
+    for (int i = 0; i < kJoin; i++) {
+      const int p = min(p0 + i, cut.parts - 1);
+      r[i] = *(const float2*)(ml + p * step);
+      v[i] = *(const f32x4_t*)(rec + p * step);
     }
-    const float inv = 1.f / L;
-    const int64_t row = (int64_t)(row0 + pair / group) * c.hq + g * group + pair % group;
-    *(u32x2_t*)(c.out + row * D + d) = u32x2_t{pack_bf2(O[0] * inv, O[1] * inv), pack_bf2(O[2] * inv, O[3] * inv)};
+    float now = M;
+#pragma unroll
+    for (int i = 0; i < kJoin; i++) now = fmaxf(now, r[i].x);
+    // a run of which the pair sees nothing left zeros and -inf
+    const float f = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M - now);
+    if (p0 > 0) {
+      L *= f;
+      O *= f;
+    }
+    M = now;
+#pragma unroll
+    for (int i = 0; i < kJoin; i++)
+      if (p0 + i < cut.parts) {
+        const float w = r[i].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(r[i].x - now);
+        L = fmaf(r[i].y, w, L);
+        O += v[i] * w;
+      }
   }
+  const float inv = 1.f / L;
+  const int64_t row = (int64_t)(row0 + pair / group) * c.hq + g * group + pair % group;
+  *(u32x2_t*)(c.out + row * D + d) = u32x2_t{pack_bf2(O[0] * inv, O[1] * inv), pack_bf2(O[2] * inv, O[3] * inv)};
 }
 
 template <int D>
 hipError_t launch_d(const AttnRowsCall& c, hipStream_t s) {
-  const Layout lay = layout_of(c.batch, c.max_rows, c.hq, c.kv.hkv, D, c.max_seq, c.num_cus, kTileRows);
-  k_attn_rows_plan<<<1, 1024, (size_t)(c.batch + 1) * sizeof(int32_t), s>>>(c, lay, kTileRows);
+  const Layout lay = layout_of(c.batch, c.max_rows, c.hq, c.kv.hkv, D, c.max_seq, c.num_cus);
+  const int waves = std::min(kPlanWaves, (std::max(c.batch, lay.tiles_cap) + 63) / 64);
+  k_attn_rows_plan<<<1, 64 * waves, (3 * (size_t)c.batch + 1) * sizeof(int32_t), s>>>(c, lay);
   const size_t lds = 2 * kRing * (size_t)kChunk * D * 2;
   if (lds > 32 * 1024) {
     const hipError_t e = hipFuncSetAttribute((const void*)k_attn_rows<D>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     if (e != hipSuccess) return e;
   }
-  k_attn_rows<D><<<(unsigned)((int64_t)lay.pairs_cap * c.kv.hkv), 256, lds, s>>>(c, lay);
-  k_attn_rows_join<D><<<dim3(lay.cuts_cap, c.kv.hkv), 256, 0, s>>>(c, lay, kTileRows);
+  k_attn_rows<D><<<(unsigned)((int64_t)lay.entries_cap * c.kv.hkv), 256, lds, s>>>(c, lay);
+  if (lay.cuts_cap > 0 && lay.recs_cap > 1)
+    k_attn_rows_join<D><<<dim3(lay.cuts_cap, c.kv.hkv, (lay.rec_rows + 1024 / D - 1) / (1024 / D)), 256, 0, s>>>(c, lay);
   return hipGetLastError();
 }
 
 }  // namespace
 
 size_t attn_rows_ws_bytes(int batch, int max_rows, int hq, int hkv, int d, int max_seq, int num_cus) {
-  return layout_of(batch, max_rows, hq, hkv, d, max_seq, num_cus, kTileRows).bytes;
+  return layout_of(batch, max_rows, hq, hkv, d, max_seq, num_cus).bytes;
 }
 
 hipError_t launch_attention_rows(const AttnRowsCall& c, hipStream_t s) {

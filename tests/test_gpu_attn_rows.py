@@ -22,7 +22,7 @@ class Case:
         self.hq, self.hkv, self.D = hq, hkv, D
         need = [-(-(c + n) // BS) for c, n in lens]
         self.nblk = nblk or sum(need) + extra_blocks
-        self.width = max(max(need), 1) + 1
+        self.width = min(max(max(need), 1) + 1, 1 << 16)
         self.h = Handle(lib, cfg_of(hq, hkv, D), max_seq or max(64, max(c + n for c, n in lens)), self.nblk, regions, fill=fill)
         rng = np.random.default_rng(seed)
         blocks = (rng.permutation(self.nblk) if place is None else np.asarray(place)).tolist()
@@ -125,6 +125,13 @@ def test_attention_rows_match_the_definition(lib, heads, lens):
 def test_attention_rows_over_long_caches(lib, heads, lens):
     """Few rows and many keys: sequences are cut into runs and joined."""
     c = Case(lib, heads, lens, seed=5)
+    close(c.run()[:c.rows], *c.want())
+    c.h.close()
+
+
+@pytest.mark.parametrize("lens", [[((1 << 20) - 3, 3)], [((1 << 20) - 1, 1)] + [(3, 1)] * 600], ids=["cut", "whole"])
+def test_attention_rows_over_the_longest_cache(lib, lens):
+    c = Case(lib, (1, 1, 64), lens, seed=6, regions=1, region=0)
     close(c.run()[:c.rows], *c.want())
     c.h.close()
 
