@@ -159,7 +159,7 @@ struct LogprobCall {
   float* top_logprobs;
   void* ws;
   // set by launch_logprobs
-  int slices = 0;
+  int segments = 0;
   void* stats = nullptr;
   void* keys = nullptr;
 };
