@@ -38,8 +38,13 @@ constexpr int kTileRows = 32 * kWaves;  // (token, head) pairs of a tile
 
 // Items (entry, KV head) the chip holds at once: two workgroups a CU.
 constexpr int kSlotsPerCu = 2;
-// A launch with fewer items than slots cuts sequences into runs of at least this many chunks.
-constexpr int kMinRun = 16;
+// A launch with fewer items than slots cuts sequences into runs of at least this many chunks, and a tile into at most this many.
+constexpr int kMinRun = 16, kMaxRuns = 32;
+// Cutting writes and reads partial outputs, so only where the longest item is this much longer than the runs would be. Whole /
+// cut, us a call on the 70B heads, longest item and run in chunks: 16 sequences of 32 rows over 500 cached 17, 16: 28 / 39; of 1 row
+// over 1000 32, 16: 32 / 26; of 32 rows over 4000 126, 63: 96 / 98; 1 of 200 rows over 2000 69, 16: 49 / 39; 4 of 100 rows over
+// 4000 129, 56: 82 / 80; 1 of 16 rows over 30000 939, 30: 480 / 46.
+constexpr float kCutFrom = 1.75f;
 
 typedef const __attribute__((address_space(4))) int32_t cint32_t;
 
@@ -49,7 +54,7 @@ struct Entry {
   int rec;        // record of a cut tile, -1 for a whole one
 };
 struct Cut {
-  int b, tile, parts, rec;
+  int row0, pairs, parts, rec;
 };
 
 // Workspace: counts, entries, cut tiles, records (o [rows][D], then m and l of each row).
@@ -235,8 +240,8 @@ __global__ void __launch_bounds__(64 * kPlanWaves) k_attn_rows_plan(AttnRowsCall
     longest = max(longest, s_longest[w]);
   }
   int run = max(longest, 1);
-  const int least = max((int)(total + slots - 1) / slots, kMinRun);
-  if (least < longest) {
+  const int least = max(max((int)(total + slots - 1) / slots, kMinRun), (longest + kMaxRuns - 1) / kMaxRuns);
+  if (longest >= kCutFrom * least) {
     const int most = max((int)(total + slots - tiles - 1) / (slots - tiles), least);
     auto try_of = [&](int j) { return least + (most - least) * j / (kTries - 1); };
     int n[kTries];
@@ -257,7 +262,7 @@ __global__ void __launch_bounds__(64 * kPlanWaves) k_attn_rows_plan(AttnRowsCall
   int runs;
   const int parts = (own.chunks + run - 1) / run, base = scan(parts, s_parts, runs);
   s_base[t] = base;
-  if (parts > 1) ((Cut*)(ws + lay.cuts))[atomicAdd(&s_cuts, 1)] = Cut{own.b, own.place, parts, base};
+  if (parts > 1) ((Cut*)(ws + lay.cuts))[atomicAdd(&s_cuts, 1)] = Cut{c.row_starts[own.b] + own.place * tm, min(tm, s_rows[own.b] - own.place * tm) * group, parts, base};
   __syncthreads();
   for (int e = t; e < runs; e += threads) {
     const int i = last_at(s_base, tiles, e);
@@ -280,10 +285,12 @@ __device__ __forceinline__ uint32_t keep_finite(uint32_t v) {
 __device__ __forceinline__ bool any_not_finite(uint32_t v) {
   return (v & 0x7f80u) == 0x7f80u || (v & 0x7f800000u) == 0x7f800000u;
 }
-// 16 bytes a lane, straight to LDS: lane l's land at dst + 16 l.
-__device__ __forceinline__ void load_lds16(const char* src, char* dst) {
-  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
-                                   (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
+// 16 bytes a lane, straight to LDS: lane l's land at dst + 16 l. once: non-temporal, nothing is left in the caches.
+__device__ __forceinline__ void load_lds16(const char* src, char* dst, bool once) {
+  const auto from = (const __attribute__((address_space(1))) void*)src;
+  const auto to = (__attribute__((address_space(3))) void*)dst;
+  if (once) __builtin_amdgcn_global_load_lds(from, to, 16, 0, 2);
+  else __builtin_amdgcn_global_load_lds(from, to, 16, 0, 0);
 }
 
 // The larger of a lane's value and its counterpart's in the other half of the wave.
@@ -313,9 +320,13 @@ __global__ void __launch_bounds__(256, 2) k_attn_rows(AttnRowsCall c, Layout lay
   cint32_t* ep = (cint32_t*)(ws + lay.entries) + (item / hkv) * 4;
   const int g = item % hkv;
   const int b = ep[0], tile = ep[1], c0 = ep[2] & 0xffff, c1 = c0 + (int)((uint32_t)ep[2] >> 16), rec = ep[3];
-  const int row0 = ((cint32_t*)c.row_starts)[b] + tile * tm;
-  const int tokens = min(tm, ((cint32_t*)c.row_starts)[b + 1] - row0);  // of this tile
-  const int first_pos = ((cint32_t*)c.ctx_lens)[b] + tile * tm;         // of its first row
+  const int seq0 = ((cint32_t*)c.row_starts)[b], seq_rows = ((cint32_t*)c.row_starts)[b + 1] - seq0;
+  const int row0 = seq0 + tile * tm;
+  const int tokens = min(tm, seq_rows - tile * tm);              // of this tile
+  const int first_pos = ((cint32_t*)c.ctx_lens)[b] + tile * tm;  // of its first row
+  // A sequence of one tile reads its keys and values once: loads that leave nothing in the caches reach more of HBM's rate (16
+  // sequences of 4 rows 67 us, 76 without), but more tiles of a sequence share what one leaves there (8192 rows 1020 us, 1054).
+  const bool once = seq_rows <= tm;
   const int kv_end = first_pos + tokens;
   const int blocks = (kv_end + kBlockTokens - 1) / kBlockTokens;
   const int32_t* bt = c.block_tables + (int64_t)b * c.max_blocks;
@@ -367,24 +378,24 @@ __global__ void __launch_bounds__(256, 2) k_attn_rows(AttnRowsCall c, Layout lay
   const uint32_t k_src = (in_block * 64 + lane) * 16;
   const uint32_t v_src = (in_block % (kBlockWaves / 2) * 64 + lane) * 32 + in_block / (kBlockWaves / 2) * 16;
   char* const mine = smem + blk_wave * kBlockBytes + in_block * 1024;  // this wave's first piece of a chunk
-  auto fetch = [&](int n, int at, const void* cache, uint32_t src, char* to) {  // n: chunk counted from c0
+  auto fetch = [&](int n, int at, const void* cache, uint32_t src, char* to, bool once) {  // n: chunk counted from c0
 #pragma unroll
     for (int j = 0; j < kPieces; j++) {
       const int from = j * (kWaves / kBlockWaves);
       const int place = __builtin_amdgcn_readlane(at, n % kGroupChunks * kChunkBlocks + from + blk_wave);
-      load_lds16((const char*)cache + (int64_t)place * kBlockBytes + src, to + from * kBlockBytes);
+      load_lds16((const char*)cache + (int64_t)place * kBlockBytes + src, to + from * kBlockBytes, once);
     }
   };
-  auto fetch_k = [&](int n, int slot) {
+  auto fetch_k = [&](int n, int slot, bool once) {
     if (n > 0 && n % kGroupChunks == 0) {
       at_k = places(ids_next);
       ids_next = load_ids(c0 + n + kGroupChunks);
     }
-    fetch(n, at_k, c.kv.k, k_src, mine + slot * kSide);
+    fetch(n, at_k, c.kv.k, k_src, mine + slot * kSide, once);
   };
-  auto fetch_v = [&](int n, int slot) {
+  auto fetch_v = [&](int n, int slot, bool once) {
     if (n % kGroupChunks == 0) at_v = at_k;
-    fetch(n, at_v, c.kv.v, v_src, mine + (kRing + slot) * kSide);
+    fetch(n, at_v, c.kv.v, v_src, mine + (kRing + slot) * kSide, once);
   };
   // Waits until this wave's loads but the last 4 * kPieces have landed (all, with `all`), then for the other waves.
   auto landed = [&](bool all) {
@@ -520,8 +531,8 @@ __global__ void __launch_bounds__(256, 2) k_attn_rows(AttnRowsCall c, Layout lay
   auto turn = [&](auto first, int n, f32x16_t& s, f32x16_t& s_next, bf16x8_t (&p_last)[2], bf16x8_t (&p)[2]) {
     constexpr bool kFirst = decltype(first)::value;
     const int ch = c0 + n, slot = n % kRing;
-    if (ch + 2 < c1) fetch_v(n + 2, (n + 2) % kRing);
-    if (ch + 4 < c1) fetch_k(n + 4, slot);
+    if (ch + 2 < c1) fetch_v(n + 2, (n + 2) % kRing, once);
+    if (ch + 4 < c1) fetch_k(n + 4, slot, once);
     if (ch * kChunk < wave_most) {
       mask(ch, s);
       products(first, slot, s, s_next, p_last, p);
@@ -534,12 +545,12 @@ __global__ void __launch_bounds__(256, 2) k_attn_rows(AttnRowsCall c, Layout lay
   f32x16_t sa, sb;
   bf16x8_t pa[2], pb[2];
   const int n_end = c1 - c0;
-  fetch_k(0, 0);
-  if (1 < n_end) fetch_k(1, 1);
-  fetch_v(0, 0);
-  if (2 < n_end) fetch_k(2, 2);
-  if (1 < n_end) fetch_v(1, 1);
-  if (3 < n_end) fetch_k(3, 3);
+  fetch_k(0, 0, once);
+  if (1 < n_end) fetch_k(1, 1, once);
+  fetch_v(0, 0, once);
+  if (2 < n_end) fetch_k(2, 2, once);
+  if (1 < n_end) fetch_v(1, 1, once);
+  if (3 < n_end) fetch_k(3, 3, once);
   landed(4 > n_end);
   if (c0 * kChunk < wave_most) {
     const char* kb = smem + k_lane;
@@ -555,21 +566,25 @@ __global__ void __launch_bounds__(256, 2) k_attn_rows(AttnRowsCall c, Layout lay
   {
     // Turns that every row of the tile sees whole and that have chunks to fetch: the same without the questions, four at a time
     // so that their places in the rings are constants.
-    auto plain = [&](auto slot, f32x16_t& s, f32x16_t& s_next, bf16x8_t (&p_last)[2], bf16x8_t (&p)[2]) {
+    auto plain = [&](auto slot, auto once, f32x16_t& s, f32x16_t& s_next, bf16x8_t (&p_last)[2], bf16x8_t (&p)[2]) {
       constexpr int kSlot = decltype(slot)::value;
-      fetch_v(n + 2, (kSlot + 2) % kRing);
-      fetch_k(n + 4, kSlot);
+      fetch_v(n + 2, (kSlot + 2) % kRing, decltype(once)::value);
+      fetch_k(n + 4, kSlot, decltype(once)::value);
       if (wave_live) products(std::false_type{}, kSlot, s, s_next, p_last, p);
       landed(false);
       n++;
     };
     const int plain_end = min(n_end - 4, (first_pos + 1) / kChunk - c0);
-    while (n + 3 < plain_end) {
-      plain(std::integral_constant<int, 1>{}, sb, sa, pa, pb);
-      plain(std::integral_constant<int, 2>{}, sa, sb, pb, pa);
-      plain(std::integral_constant<int, 3>{}, sb, sa, pa, pb);
-      plain(std::integral_constant<int, 0>{}, sa, sb, pb, pa);
-    }
+    auto turns = [&](auto once) {
+      while (n + 3 < plain_end) {
+        plain(std::integral_constant<int, 1>{}, once, sb, sa, pa, pb);
+        plain(std::integral_constant<int, 2>{}, once, sa, sb, pb, pa);
+        plain(std::integral_constant<int, 3>{}, once, sb, sa, pa, pb);
+        plain(std::integral_constant<int, 0>{}, once, sa, sb, pb, pa);
+      }
+    };
+    if (once) turns(std::true_type{});
+    else turns(std::false_type{});
   }
   for (; n < n_end; n += 2) {
     turn(std::false_type{}, n, sb, sa, pa, pb);
@@ -623,13 +638,11 @@ constexpr int kJoin = 8;
 template <int D>
 __global__ void __launch_bounds__(256) k_attn_rows_join(AttnRowsCall c, Layout lay) {
   const char* ws = (const char*)c.ws;
+  const Cut cut = ((const Cut*)(ws + lay.cuts))[blockIdx.x];  // read beside the count, and of no meaning past it
   if ((int)blockIdx.x >= ((const int32_t*)ws)[1]) return;
-  const Cut cut = ((const Cut*)(ws + lay.cuts))[blockIdx.x];
-  const int hkv = c.kv.hkv, g = blockIdx.y, group = c.hq / hkv, tm = tile_tokens(group);
-  const int row0 = c.row_starts[cut.b] + cut.tile * tm;
-  const int pairs = min(tm, c.row_starts[cut.b + 1] - row0) * group;
+  const int hkv = c.kv.hkv, g = blockIdx.y, group = c.hq / hkv;
   const int pair = blockIdx.z * (1024 / D) + threadIdx.x / (D / 4), d = threadIdx.x % (D / 4) * 4;
-  if (pair >= pairs) return;
+  if (pair >= cut.pairs) return;
   const int64_t step = (int64_t)hkv * lay.rec_rows * (D + 2);
   const float* rec = (const float*)(ws + lay.recs) + ((int64_t)cut.rec * hkv + g) * lay.rec_rows * (D + 2);
   const float* ml = rec + (int64_t)lay.rec_rows * D + 2 * pair;
@@ -664,7 +677,7 @@ __global__ void __launch_bounds__(256) k_attn_rows_join(AttnRowsCall c, Layout l
       }
   }
   const float inv = 1.f / L;
-  const int64_t row = (int64_t)(row0 + pair / group) * c.hq + g * group + pair % group;
+  const int64_t row = (int64_t)(cut.row0 + pair / group) * c.hq + g * group + pair % group;
   *(u32x2_t*)(c.out + row * D + d) = u32x2_t{pack_bf2(O[0] * inv, O[1] * inv), pack_bf2(O[2] * inv, O[3] * inv)};
 }
 
