@@ -17,68 +17,85 @@ namespace sidp {
 
 namespace {
 
-__device__ __forceinline__ int64_t wave_scan(int64_t v, int lane) {
+// Sums stop here: more rows or blocks than any call has.
+constexpr int kFull = 1 << 30;
+__device__ __forceinline__ int add_up(int a, int b) { return min(a + b, kFull); }
+
+__device__ __forceinline__ int wave_scan(int v, int lane) {
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
-    const int64_t u = __shfl_up((long long)v, o, 64);
-    if (lane >= o) v += u;
+    const int u = __shfl_up(v, o, 64);
+    if (lane >= o) v = add_up(v, u);
   }
   return v;
 }
 
 __global__ void __launch_bounds__(256) k_kv_extend(ExtendCall c) {
   extern __shared__ int32_t s_lds[];
-  int32_t* s_start = s_lds;              // [batch + 1] first row of each sequence
-  int32_t* s_block = s_lds + c.batch + 1;  // [batch] place in the free list of its first new block
-  __shared__ int64_t s_rows[4], s_blocks[4];
+  int32_t* s_start = s_lds;                // [batch + 1] first row of each sequence
+  int32_t* s_block = s_start + c.batch + 1;  // [batch] place in the free list of its first new block
+  int32_t* s_ctx = s_block + c.batch;        // [batch] its cached tokens
+  __shared__ int s_rows[4], s_blocks[4];
   __shared__ int s_all_rows, s_all_blocks;
   const int t = threadIdx.x, wave = t >> 6, lane = t & 63;
   const int per = (c.batch + 255) / 256;  // thread t sums sequences [b0, b1)
   const int b0 = min(t * per, c.batch), b1 = min(b0 + per, c.batch);
   const int taken = c.taken[0];
   // a cursor outside the list hands out nothing
-  const int64_t left = taken >= 0 && taken <= c.num_free ? c.num_free - taken : 0;
-  uint32_t bad = taken >= 0 && taken <= c.num_free ? 0u : SIDP_DEVERR_POSITION;
-  auto lengths = [&](int b, int64_t& rows, int64_t& blocks) {
-    const int64_t ctx = c.ctx_lens[b], n = c.new_lens[b];
-    const bool ok = ctx >= 0 && n >= 0 && ctx + n <= (int64_t)c.max_blocks * kBlockTokens;
-    rows = ok ? n : 0;
-    blocks = ok ? (ctx + n + kBlockTokens - 1) / kBlockTokens - (ctx + kBlockTokens - 1) / kBlockTokens : 0;
-    return ok;
+  const bool in_list = taken >= 0 && taken <= c.num_free;
+  const int left = in_list ? c.num_free - taken : 0;
+  uint32_t bad = in_list ? 0u : SIDP_DEVERR_POSITION;
+  struct Need {
+    int rows, blocks;
+    bool ok;
   };
-  int64_t rows = 0, blocks = 0;
-  for (int b = b0; b < b1; b++) {
-    int64_t r, k;
-    if (!lengths(b, r, k)) bad |= SIDP_DEVERR_POSITION;
-    rows += r;
-    blocks += k;
+  auto need_of = [&](int b) {
+    const int ctx = c.ctx_lens[b], n = c.new_lens[b];
+    s_ctx[b] = ctx;
+    const bool ok = ctx >= 0 && n >= 0 && (int64_t)ctx + n <= (int64_t)c.max_blocks * kBlockTokens;
+    const int blocks = ok ? (ctx + n + kBlockTokens - 1) / kBlockTokens - (ctx + kBlockTokens - 1) / kBlockTokens : 0;
+    return Need{ok ? n : 0, blocks, ok};
+  };
+  // a thread's first sequence stays in registers: up to 256 sequences it is its only one
+  const Need own = b0 < b1 ? need_of(b0) : Need{0, 0, true};
+  int rows = own.rows, blocks = own.blocks;
+  bool ok = own.ok;
+  for (int b = b0 + 1; b < b1; b++) {
+    const Need n = need_of(b);
+    rows = add_up(rows, n.rows);
+    blocks = add_up(blocks, n.blocks);
+    ok &= n.ok;
   }
+  if (!ok) bad |= SIDP_DEVERR_POSITION;
   if (t == 0) s_all_rows = s_all_blocks = 0;
-  int64_t rows_end = wave_scan(rows, lane), blocks_end = wave_scan(blocks, lane);
+  // exclusive sums: of the lanes before this one, then of the waves
+  const int rows_end = wave_scan(rows, lane), blocks_end = wave_scan(blocks, lane);
+  int r_at = __shfl_up(rows_end, 1, 64), k_at = __shfl_up(blocks_end, 1, 64);
+  if (lane == 0) r_at = k_at = 0;
   if (lane == 63) {
     s_rows[wave] = rows_end;
     s_blocks[wave] = blocks_end;
   }
   __syncthreads();
-  for (int w = 0; w < wave; w++) {
-    rows_end += s_rows[w];
-    blocks_end += s_blocks[w];
-  }
+#pragma unroll
+  for (int w = 0; w < 3; w++)
+    if (w < wave) {
+      r_at = add_up(r_at, s_rows[w]);
+      k_at = add_up(k_at, s_blocks[w]);
+    }
   // Sequences fit in batch order: the sums only grow, so the first that does not
-  // fit ends it for all behind it. Sums past 2^31 do not fit.
-  int64_t r_at = rows_end - rows, k_at = blocks_end - blocks;
+  // fit ends it for all behind it.
   int fit_rows = 0, fit_blocks = 0;
   for (int b = b0; b < b1; b++) {
-    int64_t r, k;
-    lengths(b, r, k);
-    s_start[b] = (int32_t)(r_at < c.max_rows ? r_at : c.max_rows);
-    s_block[b] = (int32_t)(k_at < left ? k_at : left);
-    r_at += r;
-    k_at += k;
+    const Need n = b == b0 ? own : need_of(b);
+    s_start[b] = min(r_at, c.max_rows);
+    s_block[b] = min(k_at, left);
+    r_at = add_up(r_at, n.rows);
+    k_at = add_up(k_at, n.blocks);
     if (r_at <= c.max_rows && k_at <= left) {
-      fit_rows = (int)r_at;
-      fit_blocks = (int)k_at;
-    } else if (r > 0) {
+      fit_rows = r_at;
+      fit_blocks = k_at;
+    } else if (n.rows > 0) {
       bad |= r_at > c.max_rows ? SIDP_DEVERR_POSITION : SIDP_DEVERR_NOBLOCKS;
     }
   }
@@ -91,7 +108,6 @@ __global__ void __launch_bounds__(256) k_kv_extend(ExtendCall c) {
     for (int b = t; b <= c.batch; b += 256) c.row_starts[b] = b < c.batch ? min(s_start[b], total) : total;
     if (t == 0 && c.taken_out) c.taken_out[0] = taken + s_all_blocks;
   }
-  __syncthreads();
 
   const int row = blockIdx.x * 256 + t;
   if (row < total) {
@@ -101,7 +117,7 @@ __global__ void __launch_bounds__(256) k_kv_extend(ExtendCall c) {
       if (s_start[mid] <= row) lo = mid;
       else hi = mid;
     }
-    const int ctx = c.ctx_lens[lo], pos = ctx + row - s_start[lo];
+    const int ctx = s_ctx[lo], pos = ctx + row - s_start[lo];
     const int have = (ctx + kBlockTokens - 1) / kBlockTokens, j = pos / kBlockTokens;
     int32_t* entry = c.block_tables + (int64_t)lo * c.max_blocks + j;
     int blk = j >= have ? c.free_blocks[taken + s_block[lo] + (j - have)] : *entry;
@@ -137,7 +153,7 @@ hipError_t launch_kv_extend(ExtendCall c, hipStream_t s) {
   const bool in_place = c.taken == c.taken_out;
   if (in_place) c.taken_out = nullptr;
   const int64_t groups = std::max<int64_t>(1, ((int64_t)c.max_rows + 255) / 256);
-  k_kv_extend<<<(unsigned)groups, 256, (2 * (size_t)c.batch + 1) * sizeof(int32_t), s>>>(c);
+  k_kv_extend<<<(unsigned)groups, 256, (3 * (size_t)c.batch + 1) * sizeof(int32_t), s>>>(c);
   if (in_place) k_move_cursor<<<1, 64, 0, s>>>(c.ctx_lens, c.row_starts, c.batch, const_cast<int32_t*>(c.taken));
   return hipGetLastError();
 }

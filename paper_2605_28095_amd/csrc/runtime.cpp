@@ -324,9 +324,11 @@ static int load_default_rope(sidp_handle* h) {
   const int D = h->cfg.head_dim;
   double freqs[kMaxPairs];
   for (int i = 0; i < D / 2; i++) freqs[i] = std::pow((double)h->cfg.rope_theta, -2.0 * (double)i / (double)D);
+  const int e = load_rope(h, freqs, D / 2, 1.0);
+  if (e != SIDP_OK) return e;
   h->rope_rot = D;
   h->rope_interleaved = false;
-  return load_rope(h, freqs, D / 2, 1.0);
+  return SIDP_OK;
 }
 
 int sidp_create(const sidp_config* cfg, sidp_handle** out) {
