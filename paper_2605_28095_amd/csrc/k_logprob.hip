@@ -13,8 +13,8 @@
 // 151936 fp32 logits and 20 alternatives 42 us (50 with a workgroup to every 8192
 // logits, which waited at five barriers), one row 12.5 us, launches mostly.
 //
-// Sums are kept per lane against a reference of the lane's own, which moves when a
-// score is kLazy above it. Exponents are base 2: with a_i = (x_i - m) log2 e, sum 2^a
+// Sums are kept per lane against the lane's largest logit so far: against a smaller
+// one the entropy's weighted sum would cancel. Exponents are base 2: with a_i = (x_i - m) log2 e, sum 2^a
 // and sum 2^a a give lse and the entropy. The difference comes first (one operation
 // more than a fused x_i log2 e - m log2 e): logits at the type's lowest value, as
 // masks have them, would overflow in the product.
@@ -39,7 +39,6 @@ constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kPerLane = 32;
 constexpr int kSlice = 64 * kPerLane;  // logits that a wave takes at a time
 constexpr int kCandidates = 256;       // of a wave
-constexpr float kLazy = 16.f;          // in units of the logits: weights up to e^16 keep fp32's precision
 constexpr float kLeast = -256.f;       // 2^kLeast is 0
 constexpr float kLowest = -3.40282347e+38f;  // no finite logit is lower
 // Workgroups that fill the chip: a row is cut into segments only while there are fewer rows.
@@ -227,7 +226,7 @@ __global__ void __launch_bounds__(256) k_logprob(LogprobCall c) {
     float most = piece_max[0];
 #pragma unroll
     for (int j = 1; j < kPieces; j++) most = fmaxf(most, piece_max[j]);
-    if (most > st.m + kLazy || st.m == -INFINITY) rebase(fmaxf(most, st.m), st);
+    if (most > st.m) rebase(most, st);
 
     // a NaN logit, or inf - inf, makes p and with it l NaN
     const float ref = st.m == -INFINITY ? 0.f : st.m;

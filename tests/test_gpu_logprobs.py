@@ -164,6 +164,23 @@ def test_logprobs_of_sure_and_of_large_logits(lib):
         assert np.all(np.abs(got - want) <= 2.0 ** -17 + 2.0 ** -20 * np.abs(want))
 
 
+def test_logprobs_entropy_beside_a_likely_token(lib):
+    """A token of a fifth to four fifths of the probability among many unlikely ones, at every place of a lane's share: its weight
+    may not swamp the others' in the entropy's sum."""
+    vocab, rows = 128001, 24
+    x = data(rows, vocab, 8, torch.float32, scale=2.0)[:rows * vocab].view(rows, vocab).clone()
+    targets = [(r * 5333 + 17) % vocab for r in range(rows)]
+    for r, t in enumerate(targets):
+        x[r, t] = 13.0 + r / 8
+    o = call(lib, x.flatten().cuda(), vocab, vocab, torch.tensor(targets, dtype=torch.int32, device="cuda"), 2, rows=rows)
+    lp, rank, ent, ids, lps = plain(x.double().numpy(), targets, 2)
+    assert np.array_equal(o["rank"], rank) and np.array_equal(o["ids"], ids)
+    # a lane adds 502 terms, each rounded to 2^-24 of a sum of at most 1 + 10: sqrt(502) * 11 * 2^-24 = 2^-15.9 if they all went to
+    # one lane's sums; 256 lanes share them
+    for got, want in ((o["lp"], lp), (o["ent"], ent), (o["lps"], lps)):
+        assert np.max(np.abs(got - want)) <= 2.0 ** -16
+
+
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_logprobs_of_rows_at_the_lowest_value(lib, dtype):
     """Every token at the type's lowest value is an even choice; next to it, the largest value takes all."""
