@@ -7,17 +7,20 @@
 // One pass: the logits are read once. A workgroup takes a segment of a row, its four
 // waves every fourth slice of 2048 logits of it, 32 a lane, the next slice's loads in
 // flight while one is summed up. Waves do not wait for each other until the segment
-// ends, so the pass runs at the rate of its arithmetic and loads: 2048 rows of 128001
-// bf16 logits and one alternative 104 us, 5.1 TB/s (230 before), where a copy reaches 4.9. A row's segments (as many as it takes to fill the chip when
-// rows are few, else one) are joined in index order by a second launch. 256 rows of
-// 151936 fp32 logits and 20 alternatives 42 us (50 with a workgroup to every 8192
-// logits, which waited at five barriers), one row 12.5 us, launches mostly.
+// ends. A row's segments (as many as it takes to fill the chip when rows are few, else
+// one) are joined in index order by a second launch.
+//
+// Bound by HBM where rows fill the chip: 2048 rows of 128001 bf16 logits and one
+// alternative 100 us, 5.2 TB/s, where a copy reaches 4.9 (230 us with a workgroup to
+// every 8192 logits, which waited at five barriers). 256 rows of 151936 fp32 logits and
+// 20 alternatives 40 us, 3.9 TB/s: some 5 of them are the second launch. One row 12.5 us,
+// launches mostly.
 //
 // Sums are kept per lane against the lane's largest logit so far: against a smaller
-// one the entropy's weighted sum would cancel. Exponents are base 2: with a_i = (x_i - m) log2 e, sum 2^a
-// and sum 2^a a give lse and the entropy. The difference comes first (one operation
-// more than a fused x_i log2 e - m log2 e): logits at the type's lowest value, as
-// masks have them, would overflow in the product.
+// one the entropy's weighted sum would cancel. Exponents are base 2: with
+// a_i = (x_i - m) log2 e, sum 2^a and sum 2^a a give lse and the entropy. The difference
+// comes first (one operation more than a fused x_i log2 e - m log2 e): logits at the
+// type's lowest value, as masks have them, would overflow in the product.
 //
 // The K best: the K-th largest of the 256 lanes' running maxima bounds the K-th
 // largest logit so far from below, so only logits from that bound on are kept as
@@ -41,8 +44,12 @@ constexpr int kSlice = 64 * kPerLane;  // logits that a wave takes at a time
 constexpr int kCandidates = 256;       // of a wave
 constexpr float kLeast = -256.f;       // 2^kLeast is 0
 constexpr float kLowest = -3.40282347e+38f;  // no finite logit is lower
-// Workgroups that fill the chip: a row is cut into segments only while there are fewer rows.
+// Workgroups that fill the chip: a row is cut into segments only while there are fewer rows. 256 rows of 151936 fp32 logits with
+// 256: 47 us, 512: 42, 1024: 42, 2048: 49.
 constexpr int kGroups = 512;
+// Logits of at least this many bytes are loaded past the caches: 524 MB 99.5 us (104.5 through them), 156 MB 40.1 (41.5; 40 both
+// where they were in the caches already), but 19 MB from the caches 21.2 (20.7).
+constexpr int64_t kOnceBytes = (int64_t)128 << 20;
 
 typedef unsigned long long key_t;
 
@@ -138,7 +145,8 @@ __device__ __forceinline__ void fill_up(const LogprobCall& c, int64_t row, int k
   }
 }
 
-template <bool F32>
+// ONCE: non-temporal loads.
+template <bool F32, bool ONCE>
 __global__ void __launch_bounds__(256) k_logprob(LogprobCall c) {
   constexpr int kVec = F32 ? 4 : 8;         // logits of a 16-byte piece
   constexpr int kPieces = kPerLane / kVec;  // pieces of a lane, 64 apart
@@ -193,7 +201,10 @@ __global__ void __launch_bounds__(256) k_logprob(LogprobCall c) {
     const int p0 = slice * kSlicePieces;
     if (p0 * kVec >= mis && (p0 + kSlicePieces) * kVec - mis <= c.vocab) {
 #pragma unroll
-      for (int j = 0; j < kPieces; j++) raw[j] = *(const u32x4_t*)(aligned + (uintptr_t)(p0 + j * 64 + lane) * 16);
+      for (int j = 0; j < kPieces; j++) {
+        const auto from = (const u32x4_t*)(aligned + (uintptr_t)(p0 + j * 64 + lane) * 16);
+        raw[j] = ONCE ? __builtin_nontemporal_load(from) : *from;
+      }
     } else {
 #pragma unroll
       for (int j = 0; j < kPieces; j++) raw[j] = load_piece(first_of(slice, j));
@@ -509,8 +520,9 @@ hipError_t launch_logprobs(LogprobCall c, hipStream_t s) {
   c.keys = (char*)c.ws + (size_t)c.rows * c.segments * sizeof(Stats);
   const dim3 grid((unsigned)((int64_t)c.rows * c.segments));
   const size_t lds = (size_t)c.segments * c.top * sizeof(key_t);
-  if (c.f32) k_logprob<true><<<grid, 256, 0, s>>>(c);
-  else k_logprob<false><<<grid, 256, 0, s>>>(c);
+  const bool once = (int64_t)c.rows * c.vocab * (c.f32 ? 4 : 2) >= kOnceBytes;
+  if (c.f32) once ? k_logprob<true, true><<<grid, 256, 0, s>>>(c) : k_logprob<true, false><<<grid, 256, 0, s>>>(c);
+  else once ? k_logprob<false, true><<<grid, 256, 0, s>>>(c) : k_logprob<false, false><<<grid, 256, 0, s>>>(c);
   if (c.segments > 1) {
     if (c.f32) k_logprob_join<true><<<c.rows, 256, lds, s>>>(c);
     else k_logprob_join<false><<<c.rows, 256, lds, s>>>(c);

@@ -9,7 +9,8 @@
 //    itself writes 16 or 2 bytes of each line, and lines written in parts, from
 //    workgroups on different XCDs' L2s, cost HBM a read each. A tile writes whole
 //    lines wherever its rows' slots follow each other, whatever they start at.
-// 8192 rows of the 70B heads 68 us, 5.0 TB/s (125 with a row's K and V written by the row).
+// 8192 rows of 64 and 8 heads of 128 dims 66 us, 5.1 TB/s (125 with a row's K and V written
+// by the row); 256 rows 8 us; 8 rows 3.2 us on the GPU, the launch costs more.
 #include "common.h"
 #include "internal.h"
 #include "rope.h"
@@ -19,7 +20,9 @@ namespace sidp {
 namespace {
 
 constexpr int kLongTile = 64, kShortTile = 16;
-// Calls of at least this many rows take the long tile: a short one cuts more lines, but spreads few rows over more CUs.
+// Calls of at least this many rows take the long tile: a short one cuts more lines, but spreads few rows over more CUs. They also
+// store their query rows past the caches, which leaves those to the lines of K and V: 4096 rows 29.5 us (36.4 through the caches),
+// 8192 66 (69), 2048 15.7 (15.9). Non-temporal loads as well: 8192 rows 62, but 4096 and 2048, whose source the caches hold, 33 and 19.
 constexpr int kLongRows = 2048;
 
 template <int D, bool INTERLEAVED>
@@ -36,8 +39,8 @@ __device__ __forceinline__ u32x4_t turned_head(const RopeRowsCall& c, const uint
   return turned<INTERLEAVED>(x, t);
 }
 
-// The query heads of a row, and the row's errors.
-template <int D, bool INTERLEAVED>
+// The query heads of a row, and the row's errors. ONCE: stores are non-temporal.
+template <int D, bool INTERLEAVED, bool ONCE>
 __device__ __forceinline__ void query_row(const RopeRowsCall& c, int row) {
   constexpr int kLanes = D / 8, kHeads = 256 / kLanes;
   const int sub = threadIdx.x % kLanes, pos = c.positions[row];
@@ -53,8 +56,11 @@ __device__ __forceinline__ void query_row(const RopeRowsCall& c, int row) {
   const uint16_t* src = c.qkv + (int64_t)row * c.stride;
   uint16_t* out = c.q_out + (int64_t)row * c.hq * D + sub * 8;
 #pragma unroll 4
-  for (int h = threadIdx.x / kLanes; h < c.hq; h += kHeads)
-    *(u32x4_t*)(out + h * D) = turned_head<D, INTERLEAVED>(c, src + h * D, c.g_q, sub, t);
+  for (int h = threadIdx.x / kLanes; h < c.hq; h += kHeads) {
+    const u32x4_t v = turned_head<D, INTERLEAVED>(c, src + h * D, c.g_q, sub, t);
+    if (ONCE) __builtin_nontemporal_store(v, (u32x4_t*)(out + h * D));
+    else *(u32x4_t*)(out + h * D) = v;
+  }
 }
 
 template <int D, bool INTERLEAVED, int TILE>
@@ -70,7 +76,7 @@ __global__ void __launch_bounds__(256) k_rope_rows(RopeRowsCall c, int tiles) {
   const int kv_groups = tiles * hkv;
   if ((int)blockIdx.x >= 2 * kv_groups) {
     const int row = blockIdx.x - 2 * kv_groups;
-    if (row < rows) query_row<D, INTERLEAVED>(c, row);
+    if (row < rows) query_row<D, INTERLEAVED, TILE == kLongTile>(c, row);
     return;
   }
   // tiles of one head follow each other at a distance of the heads, so that with 8 heads they share an XCD's L2
