@@ -219,6 +219,23 @@ def test_logprobs_rows_past_32_bits(lib):
     check({k: v[-2:] for k, v in o.items()}, x, [3, 3], 3)
 
 
+@pytest.mark.parametrize("dtype,vocab", [(torch.bfloat16, 64001), (torch.float32, 32003)])
+def test_logprobs_of_large_calls_are_those_of_small_ones(lib, dtype, vocab):
+    """More logits than the caches hold, in one call and in two: the same bits, and some of the rows by their definition."""
+    rows, top = 1200, 7
+    g = torch.Generator(device="cuda").manual_seed(12)
+    flat = (torch.randn(rows * vocab, generator=g, device="cuda") * 3).to(dtype)
+    flat[5 * vocab:6 * vocab:2] = -torch.inf
+    targets = torch.randint(0, vocab, (rows,), generator=g, device="cuda", dtype=torch.int32)
+    whole = call(lib, flat, vocab, vocab, targets, top, rows=rows)
+    for a in (0, rows // 2):
+        part = call(lib, flat, vocab, vocab, targets[a:a + rows // 2], top, rows=rows // 2, offset=a * vocab)
+        assert all(np.array_equal(part[k], whole[k][a:a + rows // 2], equal_nan=True) for k in whole)
+    for r in (0, 5, rows - 1):
+        x = flat[r * vocab:(r + 1) * vocab].double().cpu().numpy()[None]
+        check({k: v[r:r + 1] for k, v in whole.items()}, x, [int(targets[r])], top)
+
+
 def test_logprobs_largest_vocabulary(lib):
     vocab = 1 << 20
     flat = data(1, vocab, 6, torch.bfloat16)

@@ -110,6 +110,28 @@ def test_rope_rows_of_whole_prompts(lib, rows, start):
         assert torch.all(h.keys()[untouched.cuda()] == 3.0) and torch.all(h.values()[untouched.cuda()] == 3.0)
 
 
+@pytest.mark.parametrize("heads", [(4, 2, 64, 1), (5, 1, 128, 0)])
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+def test_rope_rows_of_long_calls_are_those_of_short_ones(lib, heads, layout):
+    """Many rows at random places in one call and in calls of a hundred: the same bits."""
+    cfg, rows, nblk = cfg_of(*heads), 2200, 150
+    with Handle(lib, cfg, 5000, nblk, fill=3.0) as h:
+        lib.sidp_set_rope(h.h, lib.make_rope(layout=layout, rotary_dim=heads[2] // 2, theta=1e4))
+        qkv, pos, slots, gq, gk = inputs(cfg, rows, nblk, 5000, 11, holes=True)
+        qkv, pos, slots, gq, gk = qkv.cuda(), dev(pos), dev(slots), gq.cuda(), gk.cuda()
+        out = torch.zeros(2, rows, heads[0], heads[2], dtype=torch.bfloat16, device="cuda")
+        lib.sidp_rope_append_rows(h.h, qkv, qkv.shape[1], rows, None, pos, slots, gq, gk, 0, out[0])
+        h.sync()
+        k, v = h.k.clone(), h.v.clone()
+        h.k.fill_(3.0)
+        h.v.fill_(3.0)
+        for a in range(0, rows, 100):
+            b = a + 100
+            lib.sidp_rope_append_rows(h.h, qkv[a:b], qkv.shape[1], 100, None, pos[a:b], slots[a:b], gq, gk, 0, out[1, a:b])
+        h.sync()
+        assert torch.equal(out[0], out[1]) and torch.equal(h.k, k) and torch.equal(h.v, v)
+
+
 @pytest.mark.parametrize("count", [-3, 0, 1, 70, 200, 1000])
 def test_rope_rows_in_use_are_read_on_the_device(lib, count):
     cfg, rows = cfg_of(4, 2, 64), 200
