@@ -17,8 +17,8 @@ namespace sidp {
 
 namespace {
 
-// Sums stop here: more rows or blocks than any call has.
-constexpr int kFull = 1 << 30;
+// Sums stop here: more rows or blocks than any call has, and twice it is still an int.
+constexpr int kFull = (1 << 30) - 1;
 __device__ __forceinline__ int add_up(int a, int b) { return min(a + b, kFull); }
 
 __device__ __forceinline__ int wave_scan(int v, int lane) {

@@ -127,6 +127,28 @@ def test_extend_out_of_rows_serves_those_before(lib, handle, max_rows):
     check(t, plain(ctx, new, free, 0, tables, 80, max_rows), len(ctx))
 
 
+@pytest.mark.parametrize("in_place", [False, True])
+def test_extend_lengths_that_sum_past_32_bits(lib, handle, in_place):
+    """The most sequences of the most tokens, 2^32 in all, behind one that fits."""
+    batch, width = lib.SIDP_EXTEND_MAX_BATCH, 65536
+    i32 = dict(dtype=torch.int32, device="cuda")
+    ctx, new = torch.zeros(batch, **i32), torch.full((batch,), 16 * width, **i32)
+    new[0] = 21
+    tables = torch.full((batch, width), -1, **i32)
+    starts, pos, slots = torch.full((batch + 2,), -99, **i32), torch.full((100,), -99, **i32), torch.full((100,), -99, **i32)
+    taken = dev([1])
+    out = taken if in_place else dev([-99])
+    lib.sidp_kv_extend(handle.h, ctx, new, batch, dev([3, 5, 7, 9]), 4, taken, out, tables, width, 100, starts, pos, slots)
+    with pytest.raises(lib.SidpError) as e:
+        handle.sync()
+    assert e.value.code == lib.SIDP_EINVAL
+    assert starts.tolist() == [0] + [21] * batch + [-99]
+    assert pos.tolist() == list(range(21)) + [-99] * 79
+    assert slots.tolist() == list(range(80, 96)) + list(range(112, 117)) + [-99] * 79
+    assert out.tolist() == [3] and tables[0, :3].tolist() == [5, 7, -1]
+    assert int((tables != -1).sum()) == 2
+
+
 def test_extend_bad_lengths_leave_the_others_served(lib, handle):
     ctx, new = [5, -1, 20, 190, 7, 2147483647, 0], [3, 4, -2, 3, 20, 2147483647, 9]  # 193 tokens: past 12 blocks
     tables, free = requests([5, 0, 20, 190, 7, 0, 0], 12, 80, 6)
