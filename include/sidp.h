@@ -545,7 +545,8 @@ int sidp_rope_frequencies(const sidp_rope *rope, int32_t head_dim, double *freqs
  * tables (double precision on the host, stored as fp32): a set-up call, not one
  * for the time between steps; no other call on the handle may overlap it, nor may
  * it be called under capture. Keys cached before keep the positions they were
- * stored with. SIDP_EINVAL as sidp_rope_frequencies. */
+ * stored with. Graphs captured before it are to be captured again: they read the new
+ * tables in the layout they were captured with. SIDP_EINVAL as sidp_rope_frequencies. */
 int sidp_set_rope(sidp_handle *h, const sidp_rope *rope);
 
 /* QK-norm (when configured), RoPE and KV append of many rows at given positions
@@ -582,8 +583,8 @@ int sidp_rope_append_rows(sidp_handle *h, const void *qkv, int64_t qkv_stride, i
  * by the lengths of the whole batch: the last bits of a row can change with the
  * other rows of the call. A sequence whose rows lie outside max_rows, or whose
  * tokens outside its table or max_seq_len, latches SIDP_EINVAL and is left out; a
- * block outside the cache latches it too and counts as zeros. P is rounded to bf16
- * before it is multiplied with V. batch 1..SIDP_EXTEND_MAX_BATCH. For one new
+ * block outside the cache latches it too, and its sequence's rows mean nothing (the
+ * others' are right). P is rounded to bf16 before it is multiplied with V. batch 1..SIDP_EXTEND_MAX_BATCH. For one new
  * token a sequence sidp_attention is the call. */
 /* 0 for sizes that sidp_attention_rows refuses, or max_rows 0. */
 size_t sidp_attention_rows_bytes(const sidp_handle *h, int32_t batch, int32_t max_rows);

@@ -101,7 +101,7 @@ struct RopeRowsCall {
   const int32_t* row_count;  // rows in use, or null
   const int32_t* positions;
   const int32_t* slots;
-  int hq, hkv;
+  int hq;
   const uint16_t* g_q;
   const uint16_t* g_k;
   float qk_eps;
@@ -113,7 +113,6 @@ struct RopeRowsCall {
   int region;
   uint16_t* q_out;
   uint32_t* err;
-  int num_cus;
 };
 hipError_t launch_rope_rows(const RopeRowsCall& c, hipStream_t s);
 

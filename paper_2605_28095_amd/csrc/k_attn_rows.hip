@@ -2,10 +2,10 @@
 // KV cache: row i of sequence b sees keys 0 .. ctx_b + i.
 //
 // A tile is the (token, query head) pairs of up to kTileRows rows that share one KV
-// head of one sequence; a workgroup takes a tile over a run of 64-token chunks. K
-// and V chunks are staged in LDS (double-buffered: the next chunk's loads are in
-// flight while this one computes), every wave holds 32 (token, head) pairs as the
-// MFMA's columns:
+// head of one sequence; a workgroup takes a tile over a run of 32-token chunks. K
+// and V go straight to LDS, into rings of four chunks each (the next two or three are
+// on their way while one is in use), and every wave holds 32 (token, head) pairs as
+// the MFMA's columns:
 //   S^T[token][pair] = K[token][:] . Q^T[:][pair]   (v_mfma_f32_32x32x16_bf16)
 //   O^T[dim][pair]  += V^T[dim][token] . P[token][pair]
 // so a pair's scores lie in two lanes and its softmax needs one exchange between
@@ -14,7 +14,17 @@
 // second product are the ones it computed. Softmax is online in base-2 units. Its
 // reference is a score of the pair, not always the largest: it only moves when a
 // chunk's weights sum to more than kMost (fp32 and bf16 have the range), so that
-// most chunks need no maximum and leave the accumulators alone.
+// most chunks need no maximum and leave the accumulators alone. The next chunk's
+// scores and the last one's values are on the matrix units while the vector units
+// exponentiate this one's.
+//
+// Bound by the matrix units where rows are many: one prompt of 8192 rows, 64 and 8
+// heads of 128 dims, 975 us, 1.13 PFLOP/s, where a library product of two 8192 x 8192
+// matrices reaches 1.22 (1444 with chunks staged through registers, 1183 straight to
+// LDS, 1039 with the turns that every row sees whole run without checks). Eight ragged
+// chunks of prompts 315 us, 1.03 PFLOP/s. By HBM where they are few: 16 sequences of 4
+// rows over up to 8191 tokens 67 us, of which 55 read the cache at 5.5 TB/s and the
+// plan and the join of cut sequences take the rest.
 //
 // P is rounded to bf16 for the second product: at most 2^-8 relative and independent from
 // key to key, so the sum is off by no more than its own rounding to bf16; the
@@ -92,7 +102,7 @@ Layout layout_of(int batch, int max_rows, int hq, int hkv, int d, int max_seq, i
 
 // Lists the items. One workgroup, a chain of latencies in front of the attention:
 // lengths are read once, into LDS, and only as many waves work as there are
-// sequences or tiles (16 sequences of 4 rows: 4 us; 9 with 16 waves).
+// sequences or tiles (16 sequences of 4 rows: 6 us; 9 with 16 waves).
 //
 // At least as many tiles as the chip holds at once: longest first, so that the
 // launch ends evenly. Fewer: every tile is cut into even runs of at most `run`

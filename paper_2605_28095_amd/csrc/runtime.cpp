@@ -1317,7 +1317,6 @@ int sidp_rope_append_rows(sidp_handle* h, const void* qkv, int64_t qkv_stride, i
   r.positions = positions;
   r.slots = slots;
   r.hq = h->cfg.num_q_heads;
-  r.hkv = h->cfg.num_kv_heads;
   r.g_q = h->cfg.qk_norm ? (const uint16_t*)g_q : nullptr;
   r.g_k = h->cfg.qk_norm ? (const uint16_t*)g_k : nullptr;
   r.qk_eps = h->cfg.qk_norm_eps;
@@ -1330,7 +1329,6 @@ int sidp_rope_append_rows(sidp_handle* h, const void* qkv, int64_t qkv_stride, i
   r.region = region;
   r.q_out = (uint16_t*)q_out;
   r.err = h->err;
-  r.num_cus = h->num_cus;
   const OnDevice on(h->device);
   HIPCHK(h, on.err);
   HIPCHK(h, launch_rope_rows(r, (hipStream_t)stream));
