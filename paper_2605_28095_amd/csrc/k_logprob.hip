@@ -4,17 +4,16 @@
 //   lse = m + log sum_i exp(x_i - m),  m = max_i x_i
 //   logprob = x_t - lse,  rank = #{i : x_i > x_t},  H = lse - sum_i p_i x_i
 //
-// One pass: the logits are read once. A workgroup takes a segment of a row, its four
-// waves every fourth slice of 2048 logits of it, 32 a lane, the next slice's loads in
+// One pass: the logits are read once. A workgroup takes a segment of a row, its 4 (or 8)
+// waves every 4th (8th) slice of 2048 logits of it, 32 a lane, the next slice's loads in
 // flight while one is summed up. Waves do not wait for each other until the segment
 // ends. A row's segments (as many as it takes to fill the chip when rows are few, else
 // one) are joined in index order by a second launch.
 //
 // Bound by HBM where rows fill the chip: 2048 rows of 128001 bf16 logits and one
-// alternative 100 us, 5.2 TB/s, where a copy reaches 4.9 (230 us with a workgroup to
-// every 8192 logits, which waited at five barriers). 256 rows of 151936 fp32 logits and
-// 20 alternatives 40 us, 3.9 TB/s: some 5 of them are the second launch. One row 12.5 us,
-// launches mostly.
+// alternative 95 us, 5.5 TB/s, where a copy reaches 4.9 (230 us with a workgroup to
+// every 8192 logits, which waited at five barriers); 256 rows of 151936 fp32 logits and
+// 20 alternatives 35 us, 4.4 TB/s. One row 11.5 us, the two launches.
 //
 // Sums are kept per lane against the lane's largest logit so far: against a smaller
 // one the entropy's weighted sum would cancel. Exponents are base 2: with
@@ -113,7 +112,7 @@ template <bool F32>
 __device__ __forceinline__ float logit_at(const LogprobCall& c, int64_t row, int i) {
   return F32 ? ((const float*)c.logits)[row * c.stride + i] : bf2f(((const uint16_t*)c.logits)[row * c.stride + i]);
 }
-template <bool F32>
+template <bool F32, int WAVES>
 __device__ __forceinline__ Row answer(const LogprobCall& c, int64_t row, const Stats& st) {
   // no distribution: a NaN or +inf among the logits (l is NaN), or nothing above -inf (l is 0)
   const Row r{st.m, logf(st.l), !(st.l > 0.f) || st.m == INFINITY};
@@ -125,7 +124,7 @@ __device__ __forceinline__ Row answer(const LogprobCall& c, int64_t row, const S
     if (c.rank) c.rank[row] = given && !r.none ? st.above : -1;
   }
   if (r.none)
-    for (int i = threadIdx.x; i < c.top; i += 256) {
+    for (int i = threadIdx.x; i < c.top; i += 64 * WAVES) {
       c.top_ids[row * c.top + i] = -1;
       c.top_logprobs[row * c.top + i] = NAN;
     }
@@ -146,17 +145,17 @@ __device__ __forceinline__ void fill_up(const LogprobCall& c, int64_t row, int k
 }
 
 // ONCE: non-temporal loads.
-template <bool F32, bool ONCE>
-__global__ void __launch_bounds__(256) k_logprob(LogprobCall c) {
+template <bool F32, bool ONCE, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES, 4) k_logprob(LogprobCall c) {
   constexpr int kVec = F32 ? 4 : 8;         // logits of a 16-byte piece
   constexpr int kPieces = kPerLane / kVec;  // pieces of a lane, 64 apart
   constexpr int kSlicePieces = 64 * kPieces;
-  __shared__ key_t s_list[4][kCandidates];
-  __shared__ key_t s_best[4 * kCandidates];
-  __shared__ Stats s_stats[4];
-  __shared__ int s_n[4];
-  __shared__ float s_tau[4];
-  __shared__ volatile float s_highest[4][64];  // each lane's largest logit
+  __shared__ key_t s_list[WAVES][kCandidates];
+  __shared__ key_t s_best[WAVES * kCandidates];
+  __shared__ Stats s_stats[WAVES];
+  __shared__ int s_n[WAVES];
+  __shared__ float s_tau[WAVES];
+  __shared__ volatile float s_highest[WAVES][64];  // each lane's largest logit
   __shared__ int s_kept;
   const int t = threadIdx.x, lane = t & 63;
   const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
@@ -223,11 +222,11 @@ __global__ void __launch_bounds__(256) k_logprob(LogprobCall c) {
 
   u32x4_t raw[kPieces];
   if (first + wave < last) load(first + wave, raw);
-  for (int slice = first + wave; slice < last; slice += 4) {
+  for (int slice = first + wave; slice < last; slice += WAVES) {
     float x[kPerLane], piece_max[kPieces];
 #pragma unroll
     for (int i = 0; i < kPerLane; i++) x[i] = value(raw[i / kVec], i % kVec);
-    if (slice + 4 < last) load(slice + 4, raw);
+    if (slice + WAVES < last) load(slice + WAVES, raw);
 #pragma unroll
     for (int j = 0; j < kPieces; j++) {
       piece_max[j] = x[j * kVec];
@@ -257,13 +256,13 @@ __global__ void __launch_bounds__(256) k_logprob(LogprobCall c) {
     highest = fmaxf(highest, most);
     done++;
     if ((done & (done - 1)) == 0) {
-      // A bound that at least `top` of the workgroup's 256 running maxima reach, by bisection between the least and the largest of
+      // A bound that at least `top` of the workgroup's lanes' running maxima reach, by bisection between the least and the largest of
       // them (to 2^-8 of their distance: a few candidates more than with the top-th largest itself, for a quarter of its price).
       // Other waves' maxima may be old ones: those hold as well, so nobody waits.
       s_highest[wave][lane] = highest;
-      float h[4], least = INFINITY, hi = -INFINITY;
+      float h[WAVES], least = INFINITY, hi = -INFINITY;
 #pragma unroll
-      for (int w = 0; w < 4; w++) {
+      for (int w = 0; w < WAVES; w++) {
         h[w] = s_highest[w][lane];
         hi = fmaxf(hi, h[w]);
         least = fminf(least, h[w] > -INFINITY ? h[w] : INFINITY);
@@ -271,7 +270,7 @@ __global__ void __launch_bounds__(256) k_logprob(LogprobCall c) {
       auto reach = [&](float v) {
         int k = 0;
 #pragma unroll
-        for (int w = 0; w < 4; w++) k += __popcll(__ballot(h[w] >= v));
+        for (int w = 0; w < WAVES; w++) k += __popcll(__ballot(h[w] >= v));
         return k;
       };
       float bound = -INFINITY;
@@ -383,13 +382,13 @@ __global__ void __launch_bounds__(256) k_logprob(LogprobCall c) {
   Stats all = s_stats[0];
   float m = all.m, bound = s_tau[0];
 #pragma unroll
-  for (int w = 1; w < 4; w++) {
+  for (int w = 1; w < WAVES; w++) {
     m = fmaxf(m, s_stats[w].m);
     bound = fmaxf(bound, s_tau[w]);  // every wave's bound holds for all
   }
   rebase(m, all);
 #pragma unroll
-  for (int w = 1; w < 4; w++) {
+  for (int w = 1; w < WAVES; w++) {
     Stats p = s_stats[w];
     rebase(m, p);
     all.l += p.l;
@@ -398,7 +397,7 @@ __global__ void __launch_bounds__(256) k_logprob(LogprobCall c) {
   }
   const bool whole = c.segments == 1;
   Row r{0.f, 0.f, false};
-  if (whole) r = answer<F32>(c, row, all);
+  if (whole) r = answer<F32, WAVES>(c, row, all);
   else if (t == 0) ((Stats*)c.stats)[blockIdx.x] = all;
   if (top == 0 || r.none) return;
   for (int i = lane; i < s_n[wave]; i += 64)
@@ -406,7 +405,7 @@ __global__ void __launch_bounds__(256) k_logprob(LogprobCall c) {
   __syncthreads();
   const int kept = s_kept;
   key_t* keys = (key_t*)c.keys + (int64_t)blockIdx.x * top;
-  for (int i = t; i < kept; i += 256) {
+  for (int i = t; i < kept; i += 64 * WAVES) {
     const key_t mine = s_best[i];
     int rank = 0;
     for (int j = 0; j < kept; j++) rank += s_best[j] > mine;
@@ -420,7 +419,7 @@ __global__ void __launch_bounds__(256) k_logprob(LogprobCall c) {
   }
   if (whole) fill_up<F32>(c, row, kept);
   else
-    for (int i = kept + t; i < top; i += 256) keys[i] = 0;  // fewer candidates in the segment than asked for
+    for (int i = kept + t; i < top; i += 64 * WAVES) keys[i] = 0;  // fewer candidates in the segment than asked for
 }
 
 // One workgroup a row. Segments are joined in index order, thread by thread.
@@ -479,7 +478,7 @@ __global__ void __launch_bounds__(256) k_logprob_join(LogprobCall c) {
   }
 #pragma unroll
   for (int w = 0; w < 4; w++) bound = s_bound[w] > bound ? s_bound[w] : bound;
-  const Row r = answer<F32>(c, row, all);
+  const Row r = answer<F32, 4>(c, row, all);
   if (c.top == 0 || r.none) return;
   for (int i = t; i < c.segments * c.top; i += 256) {
     const key_t k = keys[i];
@@ -499,30 +498,46 @@ __global__ void __launch_bounds__(256) k_logprob_join(LogprobCall c) {
   fill_up<F32>(c, row, n);
 }
 
-// Segments of a row: one while rows alone fill the chip, else enough to, of at least a slice for each of a workgroup's waves.
-int segments_of(int rows, int vocab) {
-  const int most = (vocab + 4 * kSlice - 1) / (4 * kSlice);
-  return std::min(most, (kGroups + rows - 1) / rows);
+// How a call is cut: one segment a row while rows alone fill the chip, or while workgroups of 8 waves (wide) do nearly, which
+// saves the second launch; else enough segments to, of at least a slice for each wave. Wide / two or three segments, us, fp32 of
+// 151936 and bf16 of 128001: 256 rows 35.4 / 39.6 and 27.6 / 30.5, 300 49.4 / 48.0 and 35.8 / 35.8, 500 56.6 / 62.5 and 28.1 /
+// 31.9 (no alternatives), 180 of 128001 28.8 / 30.0 and 27.3 / 27.6. From 512 rows on 4 waves: 540 rows of bf16 47.9, wide 51.4.
+struct Plan {
+  bool wide;
+  int segments;
+};
+Plan plan_of(int rows, int vocab) {
+  const int most = (vocab + 4 * kSlice - 1) / (4 * kSlice), want = (kGroups + rows - 1) / rows;
+  const bool wide = (want == 2 || want == 3) && most > 1;
+  return Plan{wide, wide ? 1 : std::min(most, want)};
 }
 
 }  // namespace
 
 size_t logprob_ws_bytes(int rows, int vocab, int top) {
-  const int segments = segments_of(rows, vocab);
+  const int segments = plan_of(rows, vocab).segments;
   // the smallest size is asked for as well: a workspace is never empty
   return std::max<size_t>(16, segments == 1 ? 0 : (size_t)rows * segments * (sizeof(Stats) + (size_t)top * sizeof(key_t)));
 }
 
 hipError_t launch_logprobs(LogprobCall c, hipStream_t s) {
   if (c.rows <= 0) return hipSuccess;
-  c.segments = segments_of(c.rows, c.vocab);
+  const Plan plan = plan_of(c.rows, c.vocab);
+  c.segments = plan.segments;
   c.stats = c.ws;
   c.keys = (char*)c.ws + (size_t)c.rows * c.segments * sizeof(Stats);
   const dim3 grid((unsigned)((int64_t)c.rows * c.segments));
   const size_t lds = (size_t)c.segments * c.top * sizeof(key_t);
   const bool once = (int64_t)c.rows * c.vocab * (c.f32 ? 4 : 2) >= kOnceBytes;
-  if (c.f32) once ? k_logprob<true, true><<<grid, 256, 0, s>>>(c) : k_logprob<true, false><<<grid, 256, 0, s>>>(c);
-  else once ? k_logprob<false, true><<<grid, 256, 0, s>>>(c) : k_logprob<false, false><<<grid, 256, 0, s>>>(c);
+  auto launch = [&](auto f32, auto past) {
+    constexpr bool F32 = decltype(f32)::value, ONCE = decltype(past)::value;
+    if (plan.wide) k_logprob<F32, ONCE, 8><<<grid, 512, 0, s>>>(c);
+    else k_logprob<F32, ONCE, 4><<<grid, 256, 0, s>>>(c);
+  };
+  const std::true_type yes;
+  const std::false_type no;
+  if (c.f32) once ? launch(yes, yes) : launch(yes, no);
+  else once ? launch(no, yes) : launch(no, no);
   if (c.segments > 1) {
     if (c.f32) k_logprob_join<true><<<c.rows, 256, lds, s>>>(c);
     else k_logprob_join<false><<<c.rows, 256, lds, s>>>(c);

@@ -236,6 +236,23 @@ def test_logprobs_of_large_calls_are_those_of_small_ones(lib, dtype, vocab):
         check({k: v[r:r + 1] for k, v in whole.items()}, x, [int(targets[r])], top)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows,vocab,stride", [(171, 8193, 8193), (300, 20011, 20024), (511, 9000, 9001)])
+@pytest.mark.parametrize("top", [0, 1, 32])
+def test_logprobs_of_hundreds_of_rows(lib, dtype, rows, vocab, stride, top):
+    """Rows that nearly fill the chip, among them masked, equal, rising and odd ones."""
+    flat = data(rows, stride, rows + top, dtype)
+    for r, what in enumerate((-torch.inf, 0.0, torch.finfo(dtype).min)):
+        flat[r * stride:r * stride + vocab] = what
+    flat[2 * stride + 77] = 1.0
+    flat[3 * stride:3 * stride + vocab] = torch.linspace(-20, 20, vocab).to(dtype)
+    flat[4 * stride:4 * stride + vocab - 3] = -torch.inf
+    flat[5 * stride + vocab - 1], flat[6 * stride + 5] = torch.nan, torch.inf
+    targets = [(r * 37) % (vocab + 2) for r in range(rows)]
+    o = call(lib, flat.cuda(), vocab, stride, torch.tensor(targets, dtype=torch.int32, device="cuda"), top, rows=rows)
+    check(o, as_rows(flat, rows, vocab, stride), targets, top)
+
+
 def test_logprobs_largest_vocabulary(lib):
     vocab = 1 << 20
     flat = data(1, vocab, 6, torch.bfloat16)
