@@ -72,6 +72,20 @@ __device__ __forceinline__ key_t wave_max_key(key_t v) {
   return v;
 }
 
+// How many of keys[0 .. n) (in LDS) are above `mine`, eight reads at a time: one after the other, each would wait for its own.
+__device__ __forceinline__ int above(const key_t* keys, int n, key_t mine) {
+  int rank = 0, j = 0;
+  for (; j + 8 <= n; j += 8) {
+    key_t k[8];
+#pragma unroll
+    for (int u = 0; u < 8; u++) k[u] = keys[j + u];
+#pragma unroll
+    for (int u = 0; u < 8; u++) rank += k[u] > mine;
+  }
+  for (; j < n; j++) rank += keys[j] > mine;
+  return rank;
+}
+
 // The largest of the wave's 64 values (none a NaN), without a trip through LDS.
 __device__ __forceinline__ float row_max(float v) {
 #define SIDP_ROR(n) \
@@ -151,7 +165,7 @@ __global__ void __launch_bounds__(64 * WAVES, 4) k_logprob(LogprobCall c) {
   constexpr int kPieces = kPerLane / kVec;  // pieces of a lane, 64 apart
   constexpr int kSlicePieces = 64 * kPieces;
   __shared__ key_t s_list[WAVES][kCandidates];
-  __shared__ key_t s_best[WAVES * kCandidates];
+  __shared__ __attribute__((aligned(16))) key_t s_best[WAVES * kCandidates];
   __shared__ Stats s_stats[WAVES];
   __shared__ int s_n[WAVES];
   __shared__ float s_tau[WAVES];
@@ -290,9 +304,14 @@ __global__ void __launch_bounds__(64 * WAVES, 4) k_logprob(LogprobCall c) {
     }
     if (!__any(most >= tau)) continue;
     if (tau_index == 0x7fffffff) {  // as nearly always
-      int count = 0;
+      int count = 0;  // at most, by pieces; counted one by one only where that is too many
 #pragma unroll
-      for (int i = 0; i < kPerLane; i++) count += __popcll(__ballot(x[i] >= tau));
+      for (int j = 0; j < kPieces; j++) count += kVec * __popcll(__ballot(piece_max[j] >= tau));
+      if (n + count > kCandidates) {
+        count = 0;
+#pragma unroll
+        for (int i = 0; i < kPerLane; i++) count += __popcll(__ballot(x[i] >= tau));
+      }
       if (n + count <= kCandidates) {
         float bound = tau;
         asm volatile("" : "+v"(bound));  // the comparisons are made again rather than kept
@@ -407,8 +426,7 @@ __global__ void __launch_bounds__(64 * WAVES, 4) k_logprob(LogprobCall c) {
   key_t* keys = (key_t*)c.keys + (int64_t)blockIdx.x * top;
   for (int i = t; i < kept; i += 64 * WAVES) {
     const key_t mine = s_best[i];
-    int rank = 0;
-    for (int j = 0; j < kept; j++) rank += s_best[j] > mine;
+    const int rank = above(s_best, kept, mine);
     if (rank >= top) continue;
     if (whole) {
       c.top_ids[row * top + rank] = key_index(mine);
@@ -480,16 +498,19 @@ __global__ void __launch_bounds__(256) k_logprob_join(LogprobCall c) {
   for (int w = 0; w < 4; w++) bound = s_bound[w] > bound ? s_bound[w] : bound;
   const Row r = answer<F32, 4>(c, row, all);
   if (c.top == 0 || r.none) return;
-  for (int i = t; i < c.segments * c.top; i += 256) {
-    const key_t k = keys[i];
-    if (k >= bound && k) s_keys[atomicAdd(&s_n, 1)] = k;
+  for (int i0 = t; i0 < c.segments * c.top; i0 += 4 * 256) {
+    key_t k[4];
+#pragma unroll
+    for (int u = 0; u < 4; u++) k[u] = i0 + u * 256 < c.segments * c.top ? keys[i0 + u * 256] : 0;
+#pragma unroll
+    for (int u = 0; u < 4; u++)
+      if (k[u] >= bound && k[u]) s_keys[atomicAdd(&s_n, 1)] = k[u];
   }
   __syncthreads();
   const int n = s_n;
   for (int i = t; i < n; i += 256) {
     const key_t mine = s_keys[i];
-    int rank = 0;
-    for (int j = 0; j < n; j++) rank += s_keys[j] > mine;
+    const int rank = above(s_keys, n, mine);
     if (rank < c.top) {
       c.top_ids[row * c.top + rank] = key_index(mine);
       c.top_logprobs[row * c.top + rank] = r.logprob(key_value(mine));
