@@ -13,7 +13,7 @@
 // Bound by HBM where rows fill the chip: 2048 rows of 128001 bf16 logits and one
 // alternative 95 us, 5.5 TB/s, where a copy reaches 4.9 (230 us with a workgroup to
 // every 8192 logits, which waited at five barriers); 256 rows of 151936 fp32 logits and
-// 20 alternatives 35 us, 4.4 TB/s. One row 11.5 us, the two launches.
+// 20 alternatives 34 us, 4.6 TB/s. One row 11.5 us, the two launches.
 //
 // Sums are kept per lane against the lane's largest logit so far: against a smaller
 // one the entropy's weighted sum would cancel. Exponents are base 2: with
