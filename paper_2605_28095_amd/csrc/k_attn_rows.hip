@@ -75,7 +75,8 @@ struct Layout {
 };
 
 __host__ __device__ inline int tile_tokens(int group) { return kTileRows / group; }
-__host__ __device__ inline int slots_of(int num_cus, int hkv) { return kSlotsPerCu * (num_cus < 1 ? 1 : num_cus) / hkv; }  // for one KV head's items
+// for one KV head's items
+__host__ __device__ inline int slots_of(int num_cus, int hkv) { return kSlotsPerCu * (num_cus < 1 ? 1 : num_cus) / hkv; }
 
 Layout layout_of(int batch, int max_rows, int hq, int hkv, int d, int max_seq, int num_cus) {
   const int group = hq / hkv, tm = tile_tokens(group), slots = slots_of(num_cus, hkv);
@@ -272,7 +273,10 @@ __global__ void __launch_bounds__(64 * kPlanWaves) k_attn_rows_plan(AttnRowsCall
   int runs;
   const int parts = (own.chunks + run - 1) / run, base = scan(parts, s_parts, runs);
   s_base[t] = base;
-  if (parts > 1) ((Cut*)(ws + lay.cuts))[atomicAdd(&s_cuts, 1)] = Cut{c.row_starts[own.b] + own.place * tm, min(tm, s_rows[own.b] - own.place * tm) * group, parts, base};
+  if (parts > 1) {
+    const int from = own.place * tm, rows = min(tm, s_rows[own.b] - from);
+    ((Cut*)(ws + lay.cuts))[atomicAdd(&s_cuts, 1)] = Cut{c.row_starts[own.b] + from, rows * group, parts, base};
+  }
   __syncthreads();
   for (int e = t; e < runs; e += threads) {
     const int i = last_at(s_base, tiles, e);
@@ -570,7 +574,8 @@ __global__ void __launch_bounds__(256, 2) k_attn_rows(AttnRowsCall c, Layout lay
 #pragma unroll
     for (int r = 0; r < 16; r++) sa[r] = 0.f;
 #pragma unroll
-    for (int kk = 0; kk < KK; kk++) sa = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(*(const u32x4_t*)(kb + kk * 512)), q[kk], sa, 0, 0, 0);
+    for (int kk = 0; kk < KK; kk++)
+      sa = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(*(const u32x4_t*)(kb + kk * 512)), q[kk], sa, 0, 0, 0);
   }
   __builtin_amdgcn_s_barrier();  // K(0) is read
   asm volatile("" ::: "memory");

@@ -6,10 +6,12 @@
 // D / 16 lanes away. Bound by latency, not bytes: 16-byte loads and stores and
 // several heads to a wave keep a launch at one round of waves on the chip (256
 // sequences of 80 heads with QK-norm 7.9 us; a wave per head, 2 bytes a lane and
-// load, 9.6); beside slot fills a wave takes a head (k_rope_append_wave). The projection output is read either as bf16 or, when the QKV
-// projection left split-K partials, reduced here: the partials are summed in
-// split order, the bias added and the result rounded to bf16, which is the
-// same value the projection's own reduction would have stored.
+// load, 9.6); beside slot fills a wave takes a head (k_rope_append_wave). The
+// projection output is read either as bf16 or, when the QKV projection left split-K
+// partials, reduced here: the partials are summed in split order, the bias added and
+// the result rounded to bf16, which is the same value the projection's own reduction
+// would have stored. Positions of another layout or part (sidp_set_rope) take the
+// general form, a wave per several heads beside fills as well.
 #include "common.h"
 #include "internal.h"
 #include "rope.h"
@@ -241,8 +243,13 @@ static hipError_t launch_rope_d(const RopeCall& c, hipStream_t s) {
   const dim3 grid(c.batch, (heads + per - 1) / per);
   const uintptr_t ptrs = (uintptr_t)c.qkv | (uintptr_t)c.bias | (uintptr_t)c.g_q | (uintptr_t)c.g_k | (uintptr_t)c.q_out;
   const bool general = c.interleaved || c.rot != D;
-  if (ptrs % 16 == 0) general ? k_rope_append<D, true, true><<<grid, 256, 0, s>>>(c) : k_rope_append<D, true, false><<<grid, 256, 0, s>>>(c);
-  else general ? k_rope_append<D, false, true><<<grid, 256, 0, s>>>(c) : k_rope_append<D, false, false><<<grid, 256, 0, s>>>(c);
+  if (ptrs % 16 == 0) {
+    if (general) k_rope_append<D, true, true><<<grid, 256, 0, s>>>(c);
+    else k_rope_append<D, true, false><<<grid, 256, 0, s>>>(c);
+  } else {
+    if (general) k_rope_append<D, false, true><<<grid, 256, 0, s>>>(c);
+    else k_rope_append<D, false, false><<<grid, 256, 0, s>>>(c);
+  }
   return hipGetLastError();
 }
 
