@@ -502,8 +502,8 @@ int sidp_attention(sidp_handle *h, const void *q, int32_t region, const int32_t 
  * Sequence b needs ceil((ctx + new) / 16) - ceil(ctx / 16) blocks more; they are
  * dealt in batch order. The first sequence whose blocks or rows do not fit into
  * free_blocks or max_rows, and every one behind it, gets no rows and no blocks
- * (row_starts tells), and sidp_sync returns SIDP_ENOBLOCKS (blocks) or
- * SIDP_EINVAL (rows). A sequence with a negative length or more tokens than its
+ * (row_starts tells), and sidp_sync returns what that first one lacked:
+ * SIDP_EINVAL if rows, SIDP_ENOBLOCKS if blocks alone. A sequence with a negative length or more tokens than its
  * table holds gets none and latches SIDP_EINVAL; the others are served. A block
  * outside the attached cache gives the slot -1 and latches SIDP_EINVAL.
  * batch 1..SIDP_EXTEND_MAX_BATCH, max_blocks_per_seq at most 65536. */

@@ -85,10 +85,12 @@ __global__ void __launch_bounds__(256) k_kv_extend(ExtendCall c) {
       k_at = add_up(k_at, s_blocks[w]);
     }
   // Sequences fit in batch order: the sums only grow, so the first that does not
-  // fit ends it for all behind it.
+  // fit ends it for all behind it, and it alone says why (what those behind it would
+  // have met says nothing: the sums go on with rows and blocks that nobody gets).
   int fit_rows = 0, fit_blocks = 0;
   for (int b = b0; b < b1; b++) {
     const Need n = b == b0 ? own : need_of(b);
+    const bool open = r_at <= c.max_rows && k_at <= left;
     s_start[b] = min(r_at, c.max_rows);
     s_block[b] = min(k_at, left);
     r_at = add_up(r_at, n.rows);
@@ -96,7 +98,7 @@ __global__ void __launch_bounds__(256) k_kv_extend(ExtendCall c) {
     if (r_at <= c.max_rows && k_at <= left) {
       fit_rows = r_at;
       fit_blocks = k_at;
-    } else if (n.rows > 0) {
+    } else if (open) {
       bad |= r_at > c.max_rows ? SIDP_DEVERR_POSITION : SIDP_DEVERR_NOBLOCKS;
     }
   }
