@@ -414,12 +414,18 @@ __global__ void __launch_bounds__(256, 2) k_attn_rows(AttnRowsCall c, Layout lay
     if (n % kGroupChunks == 0) at_v = at_k;
     fetch(n, at_v, c.kv.v, v_src, mine + (kRing + slot) * kSide, once);
   };
+  // Waits for the other waves, with no LDS operation of this one under way: what it read they may load over, what it wrote they
+  // may change.
+  auto meet = [&] {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
   // Waits until this wave's loads but the last 4 * kPieces have landed (all, with `all`), then for the other waves.
   auto landed = [&](bool all) {
     if (all) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     else asm volatile("s_waitcnt vmcnt(%0)" ::"n"(4 * kPieces) : "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
+    meet();
   };
   // The V of an edge chunk (one that the tile's first row does not see whole), landed. Tokens past kv_end become zeros (anything
   // may stand there). So do values that are not finite, for 0 * inf would reach the rows that do not see them: they are added to
@@ -446,9 +452,7 @@ __global__ void __launch_bounds__(256, 2) k_attn_rows(AttnRowsCall c, Layout lay
       }
       *(u32x4_t*)(vb + i * 16) = v;
     }
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
+    meet();
   };
 
   // K: the token of S^T's row m is m with bits 2 and 3 exchanged
@@ -577,8 +581,7 @@ __global__ void __launch_bounds__(256, 2) k_attn_rows(AttnRowsCall c, Layout lay
     for (int kk = 0; kk < KK; kk++)
       sa = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(*(const u32x4_t*)(kb + kk * 512)), q[kk], sa, 0, 0, 0);
   }
-  __builtin_amdgcn_s_barrier();  // K(0) is read
-  asm volatile("" ::: "memory");
+  meet();  // K(0) is read
   turn(std::true_type{}, 0, sa, sb, pb, pa);
   int n = 1;
   {
