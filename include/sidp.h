@@ -584,8 +584,13 @@ int sidp_rope_append_rows(sidp_handle *h, const void *qkv, int64_t qkv_stride, i
  * other rows of the call. A sequence whose rows lie outside max_rows, or whose
  * tokens outside its table or max_seq_len, latches SIDP_EINVAL and is left out; a
  * block outside the cache latches it too, and its sequence's rows mean nothing (the
- * others' are right). P is rounded to bf16 before it is multiplied with V. batch 1..SIDP_EXTEND_MAX_BATCH. For one new
- * token a sequence sidp_attention is the call. */
+ * others' are right).
+ * The softmax weights p reach V with 16 bits, as in sidp_attention, in sequences of
+ * at most 128 / (Hq / Hkv) rows (drafted tokens, single ones). In longer ones they are
+ * rounded to bf16, while their sum is not: a row is off by at most 2^-8 sum p |v|
+ * beside its own rounding, all of it to one side where scores are equal.
+ * batch 1..SIDP_EXTEND_MAX_BATCH. For one new token a sequence sidp_attention is the
+ * call. */
 /* 0 for sizes that sidp_attention_rows refuses, or max_rows 0. */
 size_t sidp_attention_rows_bytes(const sidp_handle *h, int32_t batch, int32_t max_rows);
 int sidp_attention_rows(sidp_handle *h, const void *q, int32_t region, const int32_t *row_starts,

@@ -19,16 +19,22 @@
 // exponentiate this one's.
 //
 // Bound by the matrix units where rows are many: one prompt of 8192 rows, 64 and 8
-// heads of 128 dims, 975 us, 1.13 PFLOP/s, where a library product of two 8192 x 8192
+// heads of 128 dims, 962-1000 us on several machines, 1.10-1.14 PFLOP/s, where a library product of two 8192 x 8192
 // matrices reaches 1.22 (1444 with chunks staged through registers, 1183 straight to
 // LDS, 1039 with the turns that every row sees whole run without checks). Eight ragged
-// chunks of prompts 315 us, 1.03 PFLOP/s. By HBM where they are few: 16 sequences of 4
-// rows over up to 8191 tokens 67 us, of which 55 read the cache at 5.5 TB/s and the
-// plan and the join of cut sequences take the rest.
+// chunks of prompts 301-321 us, 1.01-1.08 PFLOP/s. By HBM where they are few: 16
+// sequences of 4 rows over up to 8191 tokens 69 us, of which 57 read the cache at 5.3
+// TB/s and the plan and the join of cut sequences take the rest.
 //
-// P is rounded to bf16 for the second product: at most 2^-8 relative and independent from
-// key to key, so the sum is off by no more than its own rounding to bf16; the
-// sum of P is fp32 and unrounded.
+// The second product takes P as bf16. In a sequence of one tile (drafted tokens, single
+// ones: the calls that HBM bounds) P is cut and what the cut leaves is multiplied as well,
+// as in the attention of the decode step, so that P has 16 bits. In longer ones it is rounded:
+// the sum of P stays fp32 and unrounded, so a row is off by at most 2^-8 sum p |v| beside
+// its own rounding, all of it to one side where scores are equal. Both sides: 16 x 4
+// rows over 1-8K 67-68 us rounded, 69 in two parts; 16 rows over 30000 45 and 51; a prompt
+// of 8192 rows 985 and 1373, eight chunks 318 and 432. Distance from 64 bits, normal
+// keys, values and queries: 0.0022 of the norm rounded, 0.0016 in two parts, which is what
+// the result's own rounding makes.
 #include <type_traits>
 
 #include "common.h"
@@ -343,7 +349,8 @@ __global__ void __launch_bounds__(256, 2) k_attn_rows(AttnRowsCall c, Layout lay
   const int first_pos = ((cint32_t*)c.ctx_lens)[b] + tile * tm;  // of its first row
   // A sequence of one tile reads its keys and values once: loads that leave nothing in the caches reach more of HBM's rate (16
   // sequences of 4 rows 67 us, 76 without), but more tiles of a sequence share what one leaves there (8192 rows 1020 us, 1054).
-  const bool once = seq_rows <= tm;
+  // Beside such loads there is time for P in two parts.
+  const bool one_tile = seq_rows <= tm;
   const int kv_end = first_pos + tokens;
   const int blocks = (kv_end + kBlockTokens - 1) / kBlockTokens;
   const int32_t* bt = c.block_tables + (int64_t)b * c.max_blocks;
@@ -352,13 +359,19 @@ __global__ void __launch_bounds__(256, 2) k_attn_rows(AttnRowsCall c, Layout lay
   for (int i = t; i < 3 * D; i += 256) (&s_first[0][0])[i] = 0x7fffffff;
 
   // this lane's pair, its query, and the keys it sees
-  const int pair = wave * 32 + col;
-  const int tok = pair / group, head = pair - tok * group;
-  const bool live = tok < tokens;  // pairs past tm * group have tok >= tm
-  const int limit = live ? first_pos + tok + 1 : 0;
+  struct Pair {
+    int at, tok, head;
+  };
+  auto pair_of = [&](int thread) {
+    const int at = (thread >> 6) * 32 + (thread & 31), tok = at / group;
+    return Pair{at, tok, at - tok * group};
+  };
+  const Pair own = pair_of(t);
+  const bool live = own.tok < tokens;  // pairs past tm * group have tok >= tm
+  const int limit = live ? first_pos + own.tok + 1 : 0;
   bf16x8_t q[KK];
   {
-    const uint16_t* qp = c.q + ((int64_t)(row0 + (live ? tok : 0)) * c.hq + g * group + (live ? head : 0)) * D + half * 8;
+    const uint16_t* qp = c.q + ((int64_t)(row0 + (live ? own.tok : 0)) * c.hq + g * group + (live ? own.head : 0)) * D + half * 8;
 #pragma unroll
     for (int kk = 0; kk < KK; kk++) q[kk] = as_bf16x8(*(const u32x4_t*)(qp + kk * 16));
   }
@@ -432,7 +445,10 @@ __global__ void __launch_bounds__(256, 2) k_attn_rows(AttnRowsCall c, Layout lay
   // the others at the end, where an inf or a NaN is an inf or a NaN whenever it came.
   auto mend = [&](int ch) {
     if ((ch + 1) * kChunk <= first_pos + 1) return;
+    int t = threadIdx.x;
+    asm volatile("" : "+v"(t));  // the addresses are made here rather than kept: no register is left for them
     char* vb = smem + (kRing + (ch - c0) % kRing) * kSide;
+#pragma unroll 1
     for (int i = t; i < kSide / 16; i += 256) {
       const int t0 = ch * kChunk + i / (2 * D) * kBlockTokens + i / D % 2 * 8;
       u32x4_t v = *(const u32x4_t*)(vb + i * 16);
@@ -443,6 +459,7 @@ __global__ void __launch_bounds__(256, 2) k_attn_rows(AttnRowsCall c, Layout lay
       }
       if (any_not_finite(v[0]) || any_not_finite(v[1]) || any_not_finite(v[2]) || any_not_finite(v[3])) {
         s_odd = 1;
+#pragma unroll 1
         for (int k = 0; k < 8; k++) {
           const uint32_t h = (k & 4 ? (k & 2 ? v[3] : v[2]) : (k & 2 ? v[1] : v[0])) >> 16 * (k & 1) & 0xffffu;
           if ((h & 0x7f80u) == 0x7f80u) atomicMin(&s_first[h == 0x7f80u ? 0 : h == 0xff80u ? 1 : 2][i % D], t0 + k);
@@ -466,9 +483,27 @@ __global__ void __launch_bounds__(256, 2) k_attn_rows(AttnRowsCall c, Layout lay
       for (int r = 0; r < 16; r++) s[r] = ch * kChunk + 16 * (r / 8) + 8 * half + r % 8 < limit ? s[r] : -INFINITY;
     }
   };
+  // Eight weights as bf16: rounded, or cut (p[k]) and what the cut left (p[2 + k]). The second part gets 2^-40 of the weight more,
+  // so that it has the weight's sign too: an infinite value stays one in both products.
+  auto to_bf16 = [&](auto parts, const float* e, bf16x8_t (&p)[4], int k) {
+    uint32_t hi[4], lo[4];
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      if (decltype(parts)::value) {
+        const uint32_t a = __float_as_uint(e[2 * i]) & 0xffff0000u, b = __float_as_uint(e[2 * i + 1]) & 0xffff0000u;
+        hi[i] = a >> 16 | b;
+        lo[i] = pack_bf2(fmaf(e[2 * i], 0x1p-40f, e[2 * i] - __uint_as_float(a)),
+                         fmaf(e[2 * i + 1], 0x1p-40f, e[2 * i + 1] - __uint_as_float(b)));
+      } else {
+        hi[i] = pack_bf2(e[2 * i], e[2 * i + 1]);
+      }
+    }
+    p[k] = as_bf16x8(u32x4_t{hi[0], hi[1], hi[2], hi[3]});
+    if (decltype(parts)::value) p[2 + k] = as_bf16x8(u32x4_t{lo[0], lo[1], lo[2], lo[3]});
+  };
   // Where a pair's weights of a chunk have grown too large for its reference (or it has none): the reference moves to the chunk's
   // largest score, the sums with it, and the weights are made again.
-  auto weigh = [&](const f32x16_t& s, bf16x8_t (&p)[2], float sum) {
+  auto weigh = [&](auto parts, const f32x16_t& s, bf16x8_t (&p)[4], float sum) {
     if (__any(sum > most)) {
       float cm = s[0];
 #pragma unroll
@@ -494,24 +529,26 @@ __global__ void __launch_bounds__(256, 2) k_attn_rows(AttnRowsCall c, Layout lay
           e[r] = __builtin_amdgcn_exp2f(fmaf(s[8 * k + r], scale, base));
           sum += e[r];
         }
-        p[k] = as_bf16x8(u32x4_t{pack_bf2(e[0], e[1]), pack_bf2(e[2], e[3]), pack_bf2(e[4], e[5]), pack_bf2(e[6], e[7])});
+        to_bf16(parts, e, p, k);
       }
     }
     l += sum;
   };
-  auto add_values = [&](int slot, const bf16x8_t (&p)[2]) {
+  auto add = [&](auto parts, bf16x8_t v, const bf16x8_t (&p)[4], int k, f32x16_t& o) {
+    o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p[k], o, 0, 0, 0);
+    if (decltype(parts)::value) o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p[2 + k], o, 0, 0, 0);
+  };
+  auto add_values = [&](auto parts, int slot, const bf16x8_t (&p)[4]) {
     const char* vb = smem + (kRing + slot) * kSide + v_lane;
 #pragma unroll
     for (int k = 0; k < 2; k++)
 #pragma unroll
-      for (int dt = 0; dt < DT; dt++)
-        o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(*(const u32x4_t*)(vb + k * kBlockBytes + dt * 512)), p[k], o[dt],
-                                                        0, 0, 0);
+      for (int dt = 0; dt < DT; dt++) add(parts, as_bf16x8(*(const u32x4_t*)(vb + k * kBlockBytes + dt * 512)), p, k, o[dt]);
   };
   // Chunk ch's weights on the vector units, while the matrix units add chunk ch - 1's values (not with `first`) and make chunk
   // ch + 1's scores. Products take turns between the two, each with its share of the weights' arithmetic behind it, and fragments
   // are read kAhead products ahead. (Behind the last chunk the scores are of whatever lies there, and nobody's.)
-  auto products = [&](auto first, int slot, f32x16_t& s, f32x16_t& s_next, bf16x8_t (&p_last)[2], bf16x8_t (&p)[2]) {
+  auto products = [&](auto first, auto parts, int slot, f32x16_t& s, f32x16_t& s_next, bf16x8_t (&p_last)[4], bf16x8_t (&p)[4]) {
     constexpr bool kFirst = decltype(first)::value;
     constexpr int kProducts = KK + (kFirst ? 0 : 2 * DT), kShare = 16 / kProducts, kAhead = 3;
     const char* kb = smem + (slot + 1) % kRing * kSide + k_lane;
@@ -533,88 +570,87 @@ __global__ void __launch_bounds__(256, 2) k_attn_rows(AttnRowsCall c, Layout lay
       if (i + kAhead < kProducts) read(i + kAhead);
       const bf16x8_t f = as_bf16x8(frag[i % (kAhead + 1)]);
       if (kFirst || i % 2) s_next = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, q[kFirst ? i : i / 2], s_next, 0, 0, 0);
-      else o[i / 2 % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, p_last[i / 2 / DT], o[i / 2 % DT], 0, 0, 0);
+      else add(parts, f, p_last, i / 2 / DT, o[i / 2 % DT]);
 #pragma unroll
       for (int r = i * kShare; r < (i + 1) * kShare; r++) {
         e[r] = __builtin_amdgcn_exp2f(fmaf(s[r], scale, base));
         if (r > 0) sum += e[r - 1];  // a step late: nothing waits for the exponential
-        if (r % 8 == 7) {
-          const float* w = e + r - 7;
-          p[r / 8] = as_bf16x8(u32x4_t{pack_bf2(w[0], w[1]), pack_bf2(w[2], w[3]), pack_bf2(w[4], w[5]), pack_bf2(w[6], w[7])});
-        }
+        if (r % 8 == 7) to_bf16(parts, e + r - 7, p, r / 8);
       }
     }
     __builtin_amdgcn_sched_barrier(0);
-    weigh(s, p, sum + e[15]);
+    weigh(parts, s, p, sum + e[15]);
   };
   // A turn for chunk c0 + n: at its start V(n - 1) and K(n + 1) have landed, and V(n + 2) and K(n + 4) are fetched into the places
   // of V(n - 2) and K(n), three turns before their use.
-  auto turn = [&](auto first, int n, f32x16_t& s, f32x16_t& s_next, bf16x8_t (&p_last)[2], bf16x8_t (&p)[2]) {
-    constexpr bool kFirst = decltype(first)::value;
+  auto turn = [&](auto first, auto single, int n, f32x16_t& s, f32x16_t& s_next, bf16x8_t (&p_last)[4], bf16x8_t (&p)[4]) {
+    constexpr bool kFirst = decltype(first)::value, once = decltype(single)::value;
     const int ch = c0 + n, slot = n % kRing;
     if (ch + 2 < c1) fetch_v(n + 2, (n + 2) % kRing, once);
     if (ch + 4 < c1) fetch_k(n + 4, slot, once);
     if (ch * kChunk < wave_most) {
       mask(ch, s);
-      products(first, slot, s, s_next, p_last, p);
+      products(first, single, slot, s, s_next, p_last, p);
     } else if (!kFirst && (ch - 1) * kChunk < wave_most) {
-      add_values((n + kRing - 1) % kRing, p_last);
+      add_values(single, (n + kRing - 1) % kRing, p_last);
     }
     landed(ch + 4 >= c1);
     mend(ch);
   };
-  f32x16_t sa, sb;
-  bf16x8_t pa[2], pb[2];
-  const int n_end = c1 - c0;
-  fetch_k(0, 0, once);
-  if (1 < n_end) fetch_k(1, 1, once);
-  fetch_v(0, 0, once);
-  if (2 < n_end) fetch_k(2, 2, once);
-  if (1 < n_end) fetch_v(1, 1, once);
-  if (3 < n_end) fetch_k(3, 3, once);
-  landed(4 > n_end);
-  if (c0 * kChunk < wave_most) {
-    const char* kb = smem + k_lane;
+  // A run of chunks. single: of a sequence of one tile.
+  auto chunks = [&](auto single) {
+    constexpr bool once = decltype(single)::value;
+    f32x16_t sa, sb;
+    bf16x8_t pa[4], pb[4];
+    const int n_end = c1 - c0;
+    fetch_k(0, 0, once);
+    if (1 < n_end) fetch_k(1, 1, once);
+    fetch_v(0, 0, once);
+    if (2 < n_end) fetch_k(2, 2, once);
+    if (1 < n_end) fetch_v(1, 1, once);
+    if (3 < n_end) fetch_k(3, 3, once);
+    landed(4 > n_end);
+    if (c0 * kChunk < wave_most) {
+      const char* kb = smem + k_lane;
 #pragma unroll
-    for (int r = 0; r < 16; r++) sa[r] = 0.f;
+      for (int r = 0; r < 16; r++) sa[r] = 0.f;
 #pragma unroll
-    for (int kk = 0; kk < KK; kk++)
-      sa = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(*(const u32x4_t*)(kb + kk * 512)), q[kk], sa, 0, 0, 0);
-  }
-  meet();  // K(0) is read
-  turn(std::true_type{}, 0, sa, sb, pb, pa);
-  int n = 1;
-  {
-    // Turns that every row of the tile sees whole and that have chunks to fetch: the same without the questions, four at a time
-    // so that their places in the rings are constants.
-    auto plain = [&](auto slot, auto once, f32x16_t& s, f32x16_t& s_next, bf16x8_t (&p_last)[2], bf16x8_t (&p)[2]) {
-      constexpr int kSlot = decltype(slot)::value;
-      fetch_v(n + 2, (kSlot + 2) % kRing, decltype(once)::value);
-      fetch_k(n + 4, kSlot, decltype(once)::value);
-      if (wave_live) products(std::false_type{}, kSlot, s, s_next, p_last, p);
-      landed(false);
-      n++;
-    };
-    const int plain_end = min(n_end - 4, (first_pos + 1) / kChunk - c0);
-    auto turns = [&](auto once) {
+      for (int kk = 0; kk < KK; kk++)
+        sa = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(*(const u32x4_t*)(kb + kk * 512)), q[kk], sa, 0, 0, 0);
+    }
+    meet();  // K(0) is read
+    turn(std::true_type{}, single, 0, sa, sb, pb, pa);
+    int n = 1;
+    {
+      // Turns that every row of the tile sees whole and that have chunks to fetch: the same without the questions, four at a time
+      // so that their places in the rings are constants.
+      auto plain = [&](auto slot, f32x16_t& s, f32x16_t& s_next, bf16x8_t (&p_last)[4], bf16x8_t (&p)[4]) {
+        constexpr int kSlot = decltype(slot)::value;
+        fetch_v(n + 2, (kSlot + 2) % kRing, once);
+        fetch_k(n + 4, kSlot, once);
+        if (wave_live) products(std::false_type{}, single, kSlot, s, s_next, p_last, p);
+        landed(false);
+        n++;
+      };
+      const int plain_end = min(n_end - 4, (first_pos + 1) / kChunk - c0);
       while (n + 3 < plain_end) {
-        plain(std::integral_constant<int, 1>{}, once, sb, sa, pa, pb);
-        plain(std::integral_constant<int, 2>{}, once, sa, sb, pb, pa);
-        plain(std::integral_constant<int, 3>{}, once, sb, sa, pa, pb);
-        plain(std::integral_constant<int, 0>{}, once, sa, sb, pb, pa);
+        plain(std::integral_constant<int, 1>{}, sb, sa, pa, pb);
+        plain(std::integral_constant<int, 2>{}, sa, sb, pb, pa);
+        plain(std::integral_constant<int, 3>{}, sb, sa, pa, pb);
+        plain(std::integral_constant<int, 0>{}, sa, sb, pb, pa);
       }
-    };
-    if (once) turns(std::true_type{});
-    else turns(std::false_type{});
-  }
-  for (; n < n_end; n += 2) {
-    turn(std::false_type{}, n, sb, sa, pa, pb);
-    if (n + 1 < n_end) turn(std::false_type{}, n + 1, sa, sb, pb, pa);
-  }
-  if ((c1 - 1) * kChunk < wave_most) {
-    if (n_end & 1) add_values((n_end - 1) % kRing, pa);
-    else add_values((n_end - 1) % kRing, pb);
-  }
+    }
+    for (; n < n_end; n += 2) {
+      turn(std::false_type{}, single, n, sb, sa, pa, pb);
+      if (n + 1 < n_end) turn(std::false_type{}, single, n + 1, sa, sb, pb, pa);
+    }
+    if ((c1 - 1) * kChunk < wave_most) {
+      if (n_end & 1) add_values(single, (n_end - 1) % kRing, pa);
+      else add_values(single, (n_end - 1) % kRing, pb);
+    }
+  };
+  if (one_tile) chunks(std::true_type{});
+  else chunks(std::false_type{});
   if (bad) atomicOr(c.err, SIDP_DEVERR_BLOCK);
 
   // Register r of O^T's tile dt is dim 32 dt + 8 (r / 4) + 4 half + r % 4.
@@ -630,11 +666,15 @@ __global__ void __launch_bounds__(256, 2) k_attn_rows(AttnRowsCall c, Layout lay
       }
   }
   const float sum = l + __shfl_xor(l, 32, 64);
-  if (!live) return;
-  const int64_t out_row = (int64_t)(row0 + tok) * c.hq + g * group + head;
+  int late = threadIdx.x;
+  asm volatile("" : "+v"(late));  // made again here rather than kept
+  const Pair out = pair_of(late);
+  const int from = (late >> 5 & 1) * 4;  // the lane's first dim
+  if (out.tok >= tokens) return;
+  const int64_t out_row = (int64_t)(row0 + out.tok) * c.hq + g * group + out.head;
   if (rec < 0) {
     const float inv = 1.f / sum;
-    uint16_t* op = c.out + out_row * D + half * 4;
+    uint16_t* op = c.out + out_row * D + from;
 #pragma unroll
     for (int dt = 0; dt < DT; dt++)
 #pragma unroll
@@ -647,9 +687,9 @@ __global__ void __launch_bounds__(256, 2) k_attn_rows(AttnRowsCall c, Layout lay
     for (int dt = 0; dt < DT; dt++)
 #pragma unroll
       for (int i = 0; i < 4; i++)
-        *(f32x4_t*)(r + pair * D + dt * 32 + i * 8 + half * 4) =
+        *(f32x4_t*)(r + out.at * D + dt * 32 + i * 8 + from) =
             f32x4_t{o[dt][4 * i], o[dt][4 * i + 1], o[dt][4 * i + 2], o[dt][4 * i + 3]};
-    if (half == 0) *(float2*)(r + (int64_t)lay.rec_rows * D + 2 * pair) = make_float2(most < 0.f ? -INFINITY : -base, sum);
+    if (from == 0) *(float2*)(r + (int64_t)lay.rec_rows * D + 2 * out.at) = make_float2(most < 0.f ? -INFINITY : -base, sum);
   }
 }
 
