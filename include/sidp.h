@@ -561,7 +561,9 @@ int sidp_set_rope(sidp_handle *h, const sidp_rope *rope);
  *             negative one caches nothing (the query is still written), one past
  *             the region latches SIDP_EINVAL as well. Two rows may not share one.
  *  g_q, g_k   device bf16 [D], 16-byte aligned; read when the config has QK-norm.
- *  q_out      device bf16 [rows, Hq, D], 16-byte aligned. */
+ *  q_out      device bf16 [rows, Hq, D], 16-byte aligned.
+ * rows at most SIDP_MAX_ROWS, and with many KV heads fewer (2^24 / (1 + Hkv / 32), half
+ * a million with 992 heads): SIDP_EINVAL. */
 int sidp_rope_append_rows(sidp_handle *h, const void *qkv, int64_t qkv_stride, int32_t rows, const int32_t *row_count,
                           const int32_t *positions, const int32_t *slots, const void *g_q, const void *g_k,
                           int32_t region, void *q_out, void *stream);

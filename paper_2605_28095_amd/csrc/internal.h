@@ -114,6 +114,7 @@ struct RopeRowsCall {
   uint16_t* q_out;
   uint32_t* err;
 };
+bool rope_rows_fit(int rows, int hkv);  // in one launch
 hipError_t launch_rope_rows(const RopeRowsCall& c, hipStream_t s);
 
 // Angle per position of the rot / 2 pairs, in turning order, and the factor on

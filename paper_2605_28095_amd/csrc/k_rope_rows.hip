@@ -169,16 +169,25 @@ __global__ void __launch_bounds__(256) k_rope_rows(RopeRowsCall c, int tiles) {
   }
 }
 
+int tile_of(int rows) { return rows >= kLongRows ? kLongTile : kShortTile; }
+int64_t groups_of(int rows, int hkv) {
+  const int tile = tile_of(rows);
+  return 2 * (int64_t)((rows + tile - 1) / tile) * hkv + rows;
+}
+
 template <int D, bool INTERLEAVED>
 hipError_t launch_layout(const RopeRowsCall& c, hipStream_t s) {
-  const int tile = c.rows >= kLongRows ? kLongTile : kShortTile, tiles = (c.rows + tile - 1) / tile;
-  const unsigned grid = (unsigned)(2 * (int64_t)tiles * c.kv.hkv + c.rows);
+  const int tile = tile_of(c.rows), tiles = (c.rows + tile - 1) / tile;
+  const unsigned grid = (unsigned)groups_of(c.rows, c.kv.hkv);
   if (tile == kLongTile) k_rope_rows<D, INTERLEAVED, kLongTile><<<grid, 256, 0, s>>>(c, tiles);
   else k_rope_rows<D, INTERLEAVED, kShortTile><<<grid, 256, 0, s>>>(c, tiles);
   return hipGetLastError();
 }
 
 }  // namespace
+
+// HIP's launches have fewer than 2^32 threads.
+bool rope_rows_fit(int rows, int hkv) { return groups_of(rows, hkv) * 256 < (int64_t)1 << 32; }
 
 hipError_t launch_rope_rows(const RopeRowsCall& c, hipStream_t s) {
   if (c.rows <= 0) return hipSuccess;

@@ -1303,6 +1303,7 @@ int sidp_rope_append_rows(sidp_handle* h, const void* qkv, int64_t qkv_stride, i
                           int32_t region, void* q_out, void* stream) {
   if (!h || rows < 0 || rows > SIDP_MAX_ROWS) return SIDP_EINVAL;
   if (rows > 0 && (!qkv || !positions || !slots || !q_out)) return SIDP_EINVAL;
+  if (!rope_rows_fit(rows, h->cfg.num_kv_heads)) return SIDP_EINVAL;
   if (qkv_stride < qkv_rows(h->cfg) || qkv_stride % 8) return SIDP_EINVAL;
   if (((uintptr_t)qkv | (uintptr_t)q_out) % 16) return SIDP_EINVAL;
   if (h->cfg.qk_norm && (!g_q || !g_k || ((uintptr_t)g_q | (uintptr_t)g_k) % 16)) return SIDP_EINVAL;
