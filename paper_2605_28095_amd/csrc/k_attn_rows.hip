@@ -19,12 +19,13 @@
 // exponentiate this one's.
 //
 // Bound by the matrix units where rows are many: one prompt of 8192 rows, 64 and 8
-// heads of 128 dims, 962-1000 us on several machines, 1.10-1.14 PFLOP/s, where a library product of two 8192 x 8192
-// matrices reaches 1.22 (1444 with chunks staged through registers, 1183 straight to
-// LDS, 1039 with the turns that every row sees whole run without checks). Eight ragged
-// chunks of prompts 301-321 us, 1.01-1.08 PFLOP/s. By HBM where they are few: 16
-// sequences of 4 rows over up to 8191 tokens 69 us, of which 57 read the cache at 5.3
-// TB/s and the plan and the join of cut sequences take the rest.
+// heads of 128 dims, 962-1039 us as the machine's power lets it, 1.06-1.14 PFLOP/s, where
+// a library product of two 8192 x 8192 matrices reaches 1.22 (1444 with chunks staged
+// through registers, 1183 straight to LDS, 1039 with the turns that every row sees whole
+// run without checks, 975 on the same machine now). Eight ragged chunks of prompts
+// 301-321 us, 1.01-1.08 PFLOP/s. By HBM where they are few: 16 sequences of 4 rows over
+// up to 8191 tokens 69-70 us, of which 57 read the cache at 5.3 TB/s and the plan and the
+// join of cut sequences take the rest.
 //
 // The second product takes P as bf16. In a sequence of one tile (drafted tokens, single
 // ones: the calls that HBM bounds) P is cut and what the cut leaves is multiplied as well,
@@ -348,7 +349,7 @@ __global__ void __launch_bounds__(256, 2) k_attn_rows(AttnRowsCall c, Layout lay
   const int tokens = min(tm, seq_rows - tile * tm);              // of this tile
   const int first_pos = ((cint32_t*)c.ctx_lens)[b] + tile * tm;  // of its first row
   // A sequence of one tile reads its keys and values once: loads that leave nothing in the caches reach more of HBM's rate (16
-  // sequences of 4 rows 67 us, 76 without), but more tiles of a sequence share what one leaves there (8192 rows 1020 us, 1054).
+  // sequences of 4 rows 69 us, 77 without), but more tiles of a sequence share what one leaves there (8192 rows 1020 us, 1054).
   // Beside such loads there is time for P in two parts.
   const bool one_tile = seq_rows <= tm;
   const int kv_end = first_pos + tokens;

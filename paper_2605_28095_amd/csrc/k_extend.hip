@@ -4,8 +4,8 @@
 // of the free list in batch order; its i-th new token takes position ctx + i and
 // slot table[position / 16] * 16 + position % 16.
 //
-// Latency alone bounds it (8 bytes written a row): 1 sequence 2.4 us on the GPU, 256
-// with a token each 6.8, 512 prompts of up to 511 tokens 8.8, where a call takes 10.
+// Latency alone bounds it (8 bytes written a row): 1 sequence 2.2-2.5 us on the GPU, 256
+// with a token each 6.8-7.2, 512 prompts of up to 511 tokens 8.9-9.2, where a call takes 10.5.
 // One launch: every workgroup sums all lengths for itself (as k_attn_plan does; a
 // second launch or a wait between workgroups would cost more than re-reading 8 bytes a
 // sequence from L2), then takes 256 rows, each of which finds its sequence by bisection

@@ -21,8 +21,11 @@ namespace {
 
 constexpr int kLongTile = 64, kShortTile = 16;
 // Calls of at least this many rows take the long tile: a short one cuts more lines, but spreads few rows over more CUs. They also
-// store their query rows past the caches, which leaves those to the lines of K and V: 4096 rows 29.5 us (36.4 through the caches),
-// 8192 66 (69), 2048 15.7 (15.9). Non-temporal loads as well: 8192 rows 62, but 4096 and 2048, whose source the caches hold, 33 and 19.
+// store their query rows past the caches, which leaves those to the lines of K and V: 4096 rows 28-30 us (33-36 through the caches),
+// 8192 61-66 (65-69), 2048 15.7 (15.9). The attention then reads its queries from memory, and still the two calls behind a source
+// just written are no slower together: 8192 rows as 64 chunks 220 us (241), 8 319 (331), one prompt 1074 (1083); 4096 as 16, 4, 1
+// 151, 162, 324 (155, 161, 323); 2048 as 8, 2, 1 83, 87, 116 (82, 86, 116). Non-temporal loads as well: 8192 rows 62, but 4096 and
+// 2048, whose source the caches hold, 33 and 19.
 constexpr int kLongRows = 2048;
 
 template <int D, bool INTERLEAVED>
