@@ -32,7 +32,7 @@
 // as in the attention of the decode step, so that P has 16 bits. In longer ones it is rounded:
 // the sum of P stays fp32 and unrounded, so a row is off by at most 2^-8 sum p |v| beside
 // its own rounding, all of it to one side where scores are equal. Both sides: 16 x 4
-// rows over 1-8K 67-68 us rounded, 69 in two parts; 16 rows over 30000 45 and 51; a prompt
+// rows over 1-8K 67-68 us rounded, 69 in two parts; 16 rows over 30000 45 and 50; a prompt
 // of 8192 rows 985 and 1373, eight chunks 318 and 432. Distance from 64 bits, normal
 // keys, values and queries: 0.0022 of the norm rounded, 0.0016 in two parts, which is what
 // the result's own rounding makes.
@@ -484,17 +484,17 @@ __global__ void __launch_bounds__(256, 2) k_attn_rows(AttnRowsCall c, Layout lay
       for (int r = 0; r < 16; r++) s[r] = ch * kChunk + 16 * (r / 8) + 8 * half + r % 8 < limit ? s[r] : -INFINITY;
     }
   };
-  // Eight weights as bf16: rounded, or cut (p[k]) and what the cut left (p[2 + k]). The second part gets 2^-40 of the weight more,
-  // so that it has the weight's sign too: an infinite value stays one in both products.
+  // Eight weights as bf16: rounded, or cut (p[k]) and what the cut left (p[2 + k]). The second part gets 2^-23 of the weight more,
+  // so that it is above zero where the weight is: an infinite value stays one in both products.
   auto to_bf16 = [&](auto parts, const float* e, bf16x8_t (&p)[4], int k) {
     uint32_t hi[4], lo[4];
 #pragma unroll
     for (int i = 0; i < 4; i++) {
       if (decltype(parts)::value) {
-        const uint32_t a = __float_as_uint(e[2 * i]) & 0xffff0000u, b = __float_as_uint(e[2 * i + 1]) & 0xffff0000u;
-        hi[i] = a >> 16 | b;
-        lo[i] = pack_bf2(fmaf(e[2 * i], 0x1p-40f, e[2 * i] - __uint_as_float(a)),
-                         fmaf(e[2 * i + 1], 0x1p-40f, e[2 * i + 1] - __uint_as_float(b)));
+        const uint32_t a = __float_as_uint(e[2 * i]), b = __float_as_uint(e[2 * i + 1]);
+        hi[i] = __builtin_amdgcn_perm(b, a, 0x07060302u);  // the upper halves
+        lo[i] = pack_bf2(fmaf(e[2 * i], 1.f + 0x1p-23f, -__uint_as_float(a & 0xffff0000u)),
+                         fmaf(e[2 * i + 1], 1.f + 0x1p-23f, -__uint_as_float(b & 0xffff0000u)));
       } else {
         hi[i] = pack_bf2(e[2 * i], e[2 * i + 1]);
       }
