@@ -505,7 +505,8 @@ int sidp_attention(sidp_handle *h, const void *q, int32_t region, const int32_t 
  * (row_starts tells), and sidp_sync returns what that first one lacked:
  * SIDP_EINVAL if rows, SIDP_ENOBLOCKS if blocks alone. A sequence with a negative length or more tokens than its
  * table holds gets none and latches SIDP_EINVAL; the others are served. A block
- * outside the attached cache gives the slot -1 and latches SIDP_EINVAL.
+ * outside the attached cache (the larger one, where a bf16 and an 8-bit cache are
+ * attached) gives the slot -1 and latches SIDP_EINVAL.
  * batch 1..SIDP_EXTEND_MAX_BATCH, max_blocks_per_seq at most 65536. */
 #define SIDP_EXTEND_MAX_BATCH 4096
 int sidp_kv_extend(sidp_handle *h, const int32_t *ctx_lens, const int32_t *new_lens, int32_t batch,
@@ -567,6 +568,48 @@ int sidp_set_rope(sidp_handle *h, const sidp_rope *rope);
 int sidp_rope_append_rows(sidp_handle *h, const void *qkv, int64_t qkv_stride, int32_t rows, const int32_t *row_count,
                           const int32_t *positions, const int32_t *slots, const void *g_q, const void *g_k,
                           int32_t region, void *q_out, void *stream);
+
+/* ---- a KV cache of 8 bits ----
+ * Half the bytes of the bf16 cache a token (and 8 a token and KV head for scales):
+ * twice the sequences in the same memory, half the time of the attention that HBM
+ * bounds. The calls below read and write it; the decode step and the calls above keep
+ * to the bf16 cache. A handle may have both attached, of different sizes.
+ * Each token's D dims of a KV head are codes with one fp32 scale, K and V apart:
+ *   SIDP_KV_E4M3  code * scale, scale the least power of two with max |x| <= 448 scale
+ *                 (at least 2^-126). Relative error of an element 2^-4 at most (3 bits
+ *                 behind the leading one), however the dims differ in size, down to
+ *                 2^-6 scale, below that 2^-10 scale.
+ *   SIDP_KV_INT8  code * scale, scale = max |x| / 127 (at least 2^-126): an element is
+ *                 off by scale / 2 at most. The better one where dims are alike.
+ * Codes are rounded to nearest even from fp32. A head's dims with a NaN or an infinity
+ * among them have the scale NaN and read as NaN, all of them.
+ * Layouts:
+ *   K codes [region][block][kv_head][d / 16][token in block][d % 16]
+ *   V codes [region][block][kv_head][d][token in block]
+ *   scales  fp32 [region][block][kv_head][K, V][token in block] */
+#define SIDP_KV_E4M3 1
+#define SIDP_KV_INT8 2
+/* Bytes of one region's K codes (V's are as many) and scales; 0 for bad sizes. */
+size_t sidp_kv8_region_bytes(const sidp_config *cfg, int32_t num_phys_blocks);
+size_t sidp_kv8_scale_bytes(const sidp_config *cfg, int32_t num_phys_blocks);
+/* Registers caller-owned codes and scales of num_regions regions each, 16-byte
+ * aligned. The caller need not clear them. */
+int sidp_kv8_attach(sidp_handle *h, int32_t type, void *k_codes, void *v_codes, float *scales, int32_t num_phys_blocks,
+                    int32_t num_regions);
+/* sidp_rope_append_rows into the 8-bit cache: the same arguments, checks and queries.
+ * Keys are coded from their turned dims in fp32. */
+int sidp_rope_append_rows8(sidp_handle *h, const void *qkv, int64_t qkv_stride, int32_t rows, const int32_t *row_count,
+                           const int32_t *positions, const int32_t *slots, const void *g_q, const void *g_k,
+                           int32_t region, void *q_out, void *stream);
+/* Cached tokens as bf16 (code * scale, rounded to nearest even): row i is slot slots[i].
+ *  row_count     device int32 [1]: rows in use, at most `rows`; NULL: all.
+ *  slots         device int32 [rows], any order; a negative one leaves its row as it
+ *                was, one past the region does too and latches SIDP_EINVAL.
+ *  k_out, v_out  device bf16 [rows, Hkv, D], 16-byte aligned; either may be NULL.
+ * rows at most SIDP_MAX_ROWS, and with more than 128 KV heads fewer (2^27 / Hkv):
+ * SIDP_EINVAL. */
+int sidp_kv8_read(sidp_handle *h, int32_t region, int32_t rows, const int32_t *row_count, const int32_t *slots,
+                  void *k_out, void *v_out, void *stream);
 
 /* Causal paged GQA attention of several new tokens a sequence over region
  * `region`: for row i of sequence b (position ctx_lens[b] + i) and query head h,

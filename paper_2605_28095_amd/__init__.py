@@ -56,6 +56,7 @@ EXPORTED = [
     "sidp_set_fill_tiles", "sidp_debug_inject_hip_error", "sidp_linear_noalloc", "sidp_linear_plan",
     "sidp_attention_plan", "sidp_kv_extend", "sidp_rope_frequencies", "sidp_set_rope", "sidp_rope_append_rows",
     "sidp_attention_rows_bytes", "sidp_attention_rows", "sidp_token_logprobs_bytes", "sidp_token_logprobs",
+    "sidp_kv8_region_bytes", "sidp_kv8_scale_bytes", "sidp_kv8_attach", "sidp_rope_append_rows8", "sidp_kv8_read",
 ]
 
 SIDP_CAS_MAX_REPLICAS = 16
@@ -68,6 +69,8 @@ SIDP_LOGITS_F32 = 1
 SIDP_LOGPROBS_MAX_TOP = 32
 SIDP_LOGPROBS_MAX_VOCAB = 1 << 20
 SIDP_EXTEND_MAX_BATCH = 4096
+SIDP_KV_E4M3 = 1
+SIDP_KV_INT8 = 2
 SIDP_MAX_ROWS = 1 << 20
 
 
@@ -134,6 +137,11 @@ _sigs = {
     "sidp_pool_load_layer": (ctypes.c_int, [_P, _I, ctypes.POINTER(sidp_layer_weights), _P]),
     "sidp_kv_alloc": (ctypes.c_int, [_I, _PI, _I, _I, _I, ctypes.c_uint64, _I, _PI]),
     "sidp_kv_region_bytes": (_Z, [ctypes.POINTER(sidp_config), _I]),
+    "sidp_kv8_region_bytes": (_Z, [ctypes.POINTER(sidp_config), _I]),
+    "sidp_kv8_scale_bytes": (_Z, [ctypes.POINTER(sidp_config), _I]),
+    "sidp_kv8_attach": (ctypes.c_int, [_P, _I, _P, _P, _P, _I, _I]),
+    "sidp_rope_append_rows8": (ctypes.c_int, [_P, _P, ctypes.c_int64, _I, _P, _P, _P, _P, _P, _I, _P, _P]),
+    "sidp_kv8_read": (ctypes.c_int, [_P, _I, _I, _P, _P, _P, _P, _P]),
     "sidp_kv_attach": (ctypes.c_int, [_P, _P, _P, _I, _I]),
     "sidp_decode_step": (ctypes.c_int, [_P, _P, _P, _P, _I, _I, _I, _P, _P]),
     "sidp_sync": (ctypes.c_int, [_P]),
@@ -450,6 +458,30 @@ def sidp_rope_append_rows(h, qkv, qkv_stride, rows, row_count, positions, slots,
     _check(_lib.sidp_rope_append_rows(h, _ptr(qkv), qkv_stride, rows, _ptr(row_count), _ptr(positions), _ptr(slots),
                                       _ptr(g_q), _ptr(g_k), region, _ptr(q_out), _stream(stream)),
            "sidp_rope_append_rows")
+
+
+def sidp_kv8_region_bytes(config, num_phys_blocks):
+    return _lib.sidp_kv8_region_bytes(ctypes.byref(config), num_phys_blocks)
+
+
+def sidp_kv8_scale_bytes(config, num_phys_blocks):
+    return _lib.sidp_kv8_scale_bytes(ctypes.byref(config), num_phys_blocks)
+
+
+def sidp_kv8_attach(h, kv_type, k_codes, v_codes, scales, num_phys_blocks, num_regions):
+    _check(_lib.sidp_kv8_attach(h, kv_type, _ptr(k_codes), _ptr(v_codes), _ptr(scales), num_phys_blocks, num_regions),
+           "sidp_kv8_attach")
+
+
+def sidp_rope_append_rows8(h, qkv, qkv_stride, rows, row_count, positions, slots, g_q, g_k, region, q_out, stream=None):
+    _check(_lib.sidp_rope_append_rows8(h, _ptr(qkv), qkv_stride, rows, _ptr(row_count), _ptr(positions), _ptr(slots),
+                                       _ptr(g_q), _ptr(g_k), region, _ptr(q_out), _stream(stream)),
+           "sidp_rope_append_rows8")
+
+
+def sidp_kv8_read(h, region, rows, row_count, slots, k_out, v_out, stream=None):
+    _check(_lib.sidp_kv8_read(h, region, rows, _ptr(row_count), _ptr(slots), _ptr(k_out), _ptr(v_out), _stream(stream)),
+           "sidp_kv8_read")
 
 
 def sidp_attention_rows_bytes(h, batch, max_rows):

@@ -117,6 +117,33 @@ struct RopeRowsCall {
 bool rope_rows_fit(int rows, int hkv);  // in one launch
 hipError_t launch_rope_rows(const RopeRowsCall& c, hipStream_t s);
 
+// The 8-bit cache: codes, and the scales of each block's K and V tokens.
+struct Kv8View {
+  uint8_t* k;     // [regions][nblk][Hkv][D / 16][bs][16]
+  uint8_t* v;     // [regions][nblk][Hkv][D][bs]
+  float* scales;  // [regions][nblk][Hkv][2][bs]
+  int type;       // SIDP_KV_E4M3 or SIDP_KV_INT8
+  int nblk, regions;
+  int hkv, d;
+};
+// kv: its counts only
+struct RopeRows8Call : RopeRowsCall {
+  Kv8View kv8;
+};
+hipError_t launch_rope_rows8(const RopeRows8Call& c, hipStream_t s);
+struct Kv8ReadCall {
+  Kv8View kv8;
+  int region;
+  int rows;
+  const int32_t* row_count;
+  const int32_t* slots;
+  uint16_t* k_out;  // [rows][Hkv][D] or null
+  uint16_t* v_out;
+  uint32_t* err;
+};
+bool kv8_read_fits(int rows, int hkv);  // in one launch
+hipError_t launch_kv8_read(const Kv8ReadCall& c, hipStream_t s);
+
 // Angle per position of the rot / 2 pairs, in turning order, and the factor on
 // cos and sin (host only). False for a rope that a head of `head_dim` cannot have.
 bool rope_frequencies(const sidp_rope& r, int head_dim, double* freqs, double* scale);

@@ -88,15 +88,21 @@ __device__ __forceinline__ void load_turn(const float* cos, const float* sin, in
   }
 }
 
-// The turned dims as bf16. Every lane of the wave takes part.
+// The turned dims. Every lane of the wave takes part.
 template <bool INTERLEAVED>
-__device__ __forceinline__ u32x4_t turned(const float (&x)[8], const Turn& t) {
-  float o[8];
+__device__ __forceinline__ void turn_dims(const float (&x)[8], const Turn& t, float (&o)[8]) {
 #pragma unroll
   for (int i = 0; i < 8; i++) {
     const float other = INTERLEAVED ? x[i ^ 1] : __shfl(x[i], t.partner, 64);
     o[i] = t.on ? fmaf(x[i], t.c[i], other * t.s[i]) : x[i];
   }
+}
+
+// The same as bf16.
+template <bool INTERLEAVED>
+__device__ __forceinline__ u32x4_t turned(const float (&x)[8], const Turn& t) {
+  float o[8];
+  turn_dims<INTERLEAVED>(x, t, o);
   return u32x4_t{pack_bf2(o[0], o[1]), pack_bf2(o[2], o[3]), pack_bf2(o[4], o[5]), pack_bf2(o[6], o[7])};
 }
 

@@ -177,6 +177,7 @@ struct sidp_handle {
   uint16_t* k_cache = nullptr;
   uint16_t* v_cache = nullptr;
   int nblk = 0, regions = 0;
+  Kv8View kv8 = {};
   // library-owned device memory
   uint16_t *h = nullptr, *qkv = nullptr, *q = nullptr, *o = nullptr, *act = nullptr;
   float* ws = nullptr;
@@ -515,6 +516,26 @@ int sidp_kv_attach(sidp_handle* h, void* k_cache, void* v_cache, int32_t num_phy
   h->v_cache = (uint16_t*)v_cache;
   h->nblk = num_phys_blocks;
   h->regions = num_regions;
+  return SIDP_OK;
+}
+
+size_t sidp_kv8_region_bytes(const sidp_config* cfg, int32_t num_phys_blocks) {
+  return sidp_kv_region_bytes(cfg, num_phys_blocks) / 2;
+}
+
+size_t sidp_kv8_scale_bytes(const sidp_config* cfg, int32_t num_phys_blocks) {
+  if (!config_ok(cfg) || num_phys_blocks < 1) return 0;
+  return (size_t)num_phys_blocks * cfg->num_kv_heads * 2 * cfg->block_size * sizeof(float);
+}
+
+int sidp_kv8_attach(sidp_handle* h, int32_t type, void* k_codes, void* v_codes, float* scales, int32_t num_phys_blocks,
+                    int32_t num_regions) {
+  if (!h || !k_codes || !v_codes || !scales || num_phys_blocks < 1 || num_regions < 1) return SIDP_EINVAL;
+  if (type != SIDP_KV_E4M3 && type != SIDP_KV_INT8) return SIDP_EINVAL;
+  if (((uintptr_t)k_codes | (uintptr_t)v_codes | (uintptr_t)scales) % 16) return SIDP_EINVAL;
+  if (h->poisoned) return SIDP_ESTATE;
+  h->kv8 = Kv8View{(uint8_t*)k_codes, (uint8_t*)v_codes, scales, type, num_phys_blocks, num_regions, h->cfg.num_kv_heads,
+                   h->cfg.head_dim};
   return SIDP_OK;
 }
 
@@ -1266,7 +1287,7 @@ int sidp_kv_extend(sidp_handle* h, const int32_t* ctx_lens, const int32_t* new_l
   c.block_tables = block_tables;
   c.max_blocks = max_blocks_per_seq;
   c.max_rows = max_rows;
-  c.nblk = h->nblk > 0 ? h->nblk : 0x7fffffff / kBlockTokens;
+  c.nblk = std::max(h->nblk, h->kv8.nblk) > 0 ? std::max(h->nblk, h->kv8.nblk) : 0x7fffffff / kBlockTokens;
   c.row_starts = row_starts;
   c.positions = positions;
   c.slots = slots;
@@ -1298,9 +1319,10 @@ int sidp_set_rope(sidp_handle* h, const sidp_rope* rope) {
   return SIDP_OK;
 }
 
-int sidp_rope_append_rows(sidp_handle* h, const void* qkv, int64_t qkv_stride, int32_t rows, const int32_t* row_count,
-                          const int32_t* positions, const int32_t* slots, const void* g_q, const void* g_k,
-                          int32_t region, void* q_out, void* stream) {
+// Checks the arguments that the appends of many rows share, and fills in what does not depend on the cache.
+static int rope_rows_call(sidp_handle* h, const void* qkv, int64_t qkv_stride, int32_t rows, const int32_t* row_count,
+                          const int32_t* positions, const int32_t* slots, const void* g_q, const void* g_k, void* q_out,
+                          RopeRowsCall* r) {
   if (!h || rows < 0 || rows > SIDP_MAX_ROWS) return SIDP_EINVAL;
   if (rows > 0 && (!qkv || !positions || !slots || !q_out)) return SIDP_EINVAL;
   if (!rope_rows_fit(rows, h->cfg.num_kv_heads)) return SIDP_EINVAL;
@@ -1308,31 +1330,71 @@ int sidp_rope_append_rows(sidp_handle* h, const void* qkv, int64_t qkv_stride, i
   if (((uintptr_t)qkv | (uintptr_t)q_out) % 16) return SIDP_EINVAL;
   if (h->cfg.qk_norm && (!g_q || !g_k || ((uintptr_t)g_q | (uintptr_t)g_k) % 16)) return SIDP_EINVAL;
   if (h->poisoned) return SIDP_ESTATE;
+  r->qkv = (const uint16_t*)qkv;
+  r->stride = qkv_stride;
+  r->rows = rows;
+  r->row_count = row_count;
+  r->positions = positions;
+  r->slots = slots;
+  r->hq = h->cfg.num_q_heads;
+  r->g_q = h->cfg.qk_norm ? (const uint16_t*)g_q : nullptr;
+  r->g_k = h->cfg.qk_norm ? (const uint16_t*)g_k : nullptr;
+  r->qk_eps = h->cfg.qk_norm_eps;
+  r->rope_cos = h->rope_cos;
+  r->rope_sin = h->rope_sin;
+  r->max_seq = h->cfg.max_seq_len;
+  r->rot = h->rope_rot;
+  r->interleaved = h->rope_interleaved;
+  r->kv = kv_view(h);
+  r->q_out = (uint16_t*)q_out;
+  r->err = h->err;
+  return SIDP_OK;
+}
+
+int sidp_rope_append_rows(sidp_handle* h, const void* qkv, int64_t qkv_stride, int32_t rows, const int32_t* row_count,
+                          const int32_t* positions, const int32_t* slots, const void* g_q, const void* g_k,
+                          int32_t region, void* q_out, void* stream) {
+  RopeRowsCall r;
+  const int bad = rope_rows_call(h, qkv, qkv_stride, rows, row_count, positions, slots, g_q, g_k, q_out, &r);
+  if (bad != SIDP_OK) return bad;
   if (!h->k_cache) return SIDP_ESTATE;
   if (region < 0 || region >= h->regions) return SIDP_EINVAL;
-  RopeRowsCall r;
-  r.qkv = (const uint16_t*)qkv;
-  r.stride = qkv_stride;
-  r.rows = rows;
-  r.row_count = row_count;
-  r.positions = positions;
-  r.slots = slots;
-  r.hq = h->cfg.num_q_heads;
-  r.g_q = h->cfg.qk_norm ? (const uint16_t*)g_q : nullptr;
-  r.g_k = h->cfg.qk_norm ? (const uint16_t*)g_k : nullptr;
-  r.qk_eps = h->cfg.qk_norm_eps;
-  r.rope_cos = h->rope_cos;
-  r.rope_sin = h->rope_sin;
-  r.max_seq = h->cfg.max_seq_len;
-  r.rot = h->rope_rot;
-  r.interleaved = h->rope_interleaved;
-  r.kv = kv_view(h);
   r.region = region;
-  r.q_out = (uint16_t*)q_out;
-  r.err = h->err;
   const OnDevice on(h->device);
   HIPCHK(h, on.err);
   HIPCHK(h, launch_rope_rows(r, (hipStream_t)stream));
+  return SIDP_OK;
+}
+
+int sidp_rope_append_rows8(sidp_handle* h, const void* qkv, int64_t qkv_stride, int32_t rows, const int32_t* row_count,
+                           const int32_t* positions, const int32_t* slots, const void* g_q, const void* g_k,
+                           int32_t region, void* q_out, void* stream) {
+  RopeRows8Call r;
+  const int bad = rope_rows_call(h, qkv, qkv_stride, rows, row_count, positions, slots, g_q, g_k, q_out, &r);
+  if (bad != SIDP_OK) return bad;
+  if (!h->kv8.k) return SIDP_ESTATE;
+  if (region < 0 || region >= h->kv8.regions) return SIDP_EINVAL;
+  r.region = region;
+  r.kv8 = h->kv8;
+  r.kv.nblk = h->kv8.nblk;
+  const OnDevice on(h->device);
+  HIPCHK(h, on.err);
+  HIPCHK(h, launch_rope_rows8(r, (hipStream_t)stream));
+  return SIDP_OK;
+}
+
+int sidp_kv8_read(sidp_handle* h, int32_t region, int32_t rows, const int32_t* row_count, const int32_t* slots, void* k_out,
+                  void* v_out, void* stream) {
+  if (!h || rows < 0 || rows > SIDP_MAX_ROWS || !kv8_read_fits(rows, h->cfg.num_kv_heads)) return SIDP_EINVAL;
+  if (rows > 0 && (!slots || (!k_out && !v_out))) return SIDP_EINVAL;
+  if (((uintptr_t)k_out | (uintptr_t)v_out) % 16) return SIDP_EINVAL;
+  if (h->poisoned) return SIDP_ESTATE;
+  if (!h->kv8.k) return SIDP_ESTATE;
+  if (region < 0 || region >= h->kv8.regions) return SIDP_EINVAL;
+  const Kv8ReadCall c = {h->kv8, region, rows, row_count, slots, (uint16_t*)k_out, (uint16_t*)v_out, h->err};
+  const OnDevice on(h->device);
+  HIPCHK(h, on.err);
+  HIPCHK(h, launch_kv8_read(c, (hipStream_t)stream));
   return SIDP_OK;
 }
 
