@@ -642,6 +642,49 @@ int sidp_attention_rows(sidp_handle *h, const void *q, int32_t region, const int
                         const int32_t *ctx_lens, const int32_t *block_tables, int32_t max_blocks_per_seq, int32_t batch,
                         int32_t max_rows, void *out, void *workspace, size_t workspace_bytes, void *stream);
 
+/* sidp_attention_rows over the 8-bit cache: the same arguments, order of keys, errors
+ * and sharing of the work, with a workspace of sidp_attention_rows8_bytes. Codes are
+ * multiplied as they are (bf16 holds them), the scale of a key's token with its
+ * scores and the scale of a value's token with its weights in fp32, so that the cache's
+ * own rounding is the only one beside those of sidp_attention_rows. A row that sees a
+ * token without a scale (NaN) is NaN. More rows and heads than one launch covers (2^24
+ * items of 128 / (Hq / Hkv) rows of a sequence and a KV head) are SIDP_EINVAL, and their
+ * size is 0. */
+size_t sidp_attention_rows8_bytes(const sidp_handle *h, int32_t batch, int32_t max_rows);
+int sidp_attention_rows8(sidp_handle *h, const void *q, int32_t region, const int32_t *row_starts,
+                         const int32_t *ctx_lens, const int32_t *block_tables, int32_t max_blocks_per_seq, int32_t batch,
+                         int32_t max_rows, void *out, void *workspace, size_t workspace_bytes, void *stream);
+
+/* sidp_attention_rows for sequences of which groups have the same leading tokens in the
+ * same blocks (answers to one prompt, requests under one instruction): those keys and
+ * values are read once for the whole group, whose rows are multiplied with them
+ * together. The arguments of sidp_attention_rows, and
+ *  cache         SIDP_CACHE_BF16 (sidp_kv_attach) or SIDP_CACHE_8BIT (sidp_kv8_attach).
+ *  group_starts  device int32 [groups + 1]: group i is the sequences group_starts[i] ..
+ *                group_starts[i + 1] - 1; those of no group share nothing.
+ *  shared_lens   device int32 [groups]: cached tokens that the group's sequences have in
+ *                common, at most ctx_lens of each that has rows. Their block tables hold
+ *                the same blocks for them; the kernels read one sequence's.
+ *  groups        0 .. batch; 0: none.
+ * Whole chunks of 32 shared tokens are read once, the rest by each sequence as its own;
+ * so is everything where it does not pay: a group of which the rows fill no fewer than
+ * half as many tiles of 128 / (Hq / Hkv) rows together as each sequence by itself, or of
+ * under 128 shared tokens. The result is that of sidp_attention_rows but for its last
+ * bits; the softmax weights of shared tokens reach V with 16 bits in groups of at most
+ * 128 / (Hq / Hkv) rows, rounded to bf16 in larger ones.
+ * Groups out of order or range, or with a negative length, latch SIDP_EINVAL, as does a
+ * shared length past a sequence's own: the rows are right, and nothing is shared (of
+ * that group in the second case). A sequence that sidp_attention_rows leaves out is left
+ * out here, and then nothing is shared in the call. Sizes past one launch are refused
+ * as sidp_attention_rows8 does, at two thirds as many items. */
+#define SIDP_CACHE_BF16 0
+#define SIDP_CACHE_8BIT 1
+size_t sidp_attention_shared_bytes(const sidp_handle *h, int32_t cache, int32_t batch, int32_t max_rows);
+int sidp_attention_shared(sidp_handle *h, int32_t cache, const void *q, int32_t region, const int32_t *group_starts,
+                          const int32_t *shared_lens, int32_t groups, const int32_t *row_starts, const int32_t *ctx_lens,
+                          const int32_t *block_tables, int32_t max_blocks_per_seq, int32_t batch, int32_t max_rows, void *out,
+                          void *workspace, size_t workspace_bytes, void *stream);
+
 /* ---- answers ----
  * Log probabilities of given tokens, their ranks, the entropy and the most likely
  * tokens of each row of logits (the output projection of sidp_linear, say), on the

@@ -57,6 +57,7 @@ EXPORTED = [
     "sidp_attention_plan", "sidp_kv_extend", "sidp_rope_frequencies", "sidp_set_rope", "sidp_rope_append_rows",
     "sidp_attention_rows_bytes", "sidp_attention_rows", "sidp_token_logprobs_bytes", "sidp_token_logprobs",
     "sidp_kv8_region_bytes", "sidp_kv8_scale_bytes", "sidp_kv8_attach", "sidp_rope_append_rows8", "sidp_kv8_read",
+    "sidp_attention_rows8_bytes", "sidp_attention_rows8", "sidp_attention_shared_bytes", "sidp_attention_shared",
 ]
 
 SIDP_CAS_MAX_REPLICAS = 16
@@ -71,6 +72,8 @@ SIDP_LOGPROBS_MAX_VOCAB = 1 << 20
 SIDP_EXTEND_MAX_BATCH = 4096
 SIDP_KV_E4M3 = 1
 SIDP_KV_INT8 = 2
+SIDP_CACHE_BF16 = 0
+SIDP_CACHE_8BIT = 1
 SIDP_MAX_ROWS = 1 << 20
 
 
@@ -137,6 +140,10 @@ _sigs = {
     "sidp_pool_load_layer": (ctypes.c_int, [_P, _I, ctypes.POINTER(sidp_layer_weights), _P]),
     "sidp_kv_alloc": (ctypes.c_int, [_I, _PI, _I, _I, _I, ctypes.c_uint64, _I, _PI]),
     "sidp_kv_region_bytes": (_Z, [ctypes.POINTER(sidp_config), _I]),
+    "sidp_attention_rows8_bytes": (_Z, [_P, _I, _I]),
+    "sidp_attention_rows8": (ctypes.c_int, [_P, _P, _I, _P, _P, _P, _I, _I, _I, _P, _P, _Z, _P]),
+    "sidp_attention_shared_bytes": (_Z, [_P, _I, _I, _I]),
+    "sidp_attention_shared": (ctypes.c_int, [_P, _I, _P, _I, _P, _P, _I, _P, _P, _P, _I, _I, _I, _P, _P, _Z, _P]),
     "sidp_kv8_region_bytes": (_Z, [ctypes.POINTER(sidp_config), _I]),
     "sidp_kv8_scale_bytes": (_Z, [ctypes.POINTER(sidp_config), _I]),
     "sidp_kv8_attach": (ctypes.c_int, [_P, _I, _P, _P, _P, _I, _I]),
@@ -493,6 +500,29 @@ def sidp_attention_rows(h, q, region, row_starts, ctx_lens, block_tables, max_bl
     _check(_lib.sidp_attention_rows(h, _ptr(q), region, _ptr(row_starts), _ptr(ctx_lens), _ptr(block_tables),
                                     max_blocks_per_seq, batch, max_rows, _ptr(out), _ptr(workspace), workspace_bytes,
                                     _stream(stream)), "sidp_attention_rows")
+
+
+def sidp_attention_rows8_bytes(h, batch, max_rows):
+    return _lib.sidp_attention_rows8_bytes(h, batch, max_rows)
+
+
+def sidp_attention_rows8(h, q, region, row_starts, ctx_lens, block_tables, max_blocks_per_seq, batch, max_rows, out,
+                         workspace, workspace_bytes, stream=None):
+    _check(_lib.sidp_attention_rows8(h, _ptr(q), region, _ptr(row_starts), _ptr(ctx_lens), _ptr(block_tables),
+                                     max_blocks_per_seq, batch, max_rows, _ptr(out), _ptr(workspace), workspace_bytes,
+                                     _stream(stream)), "sidp_attention_rows8")
+
+
+def sidp_attention_shared_bytes(h, cache, batch, max_rows):
+    return _lib.sidp_attention_shared_bytes(h, cache, batch, max_rows)
+
+
+def sidp_attention_shared(h, cache, q, region, group_starts, shared_lens, groups, row_starts, ctx_lens, block_tables,
+                          max_blocks_per_seq, batch, max_rows, out, workspace, workspace_bytes, stream=None):
+    _check(_lib.sidp_attention_shared(h, cache, _ptr(q), region, _ptr(group_starts), _ptr(shared_lens), groups,
+                                      _ptr(row_starts), _ptr(ctx_lens), _ptr(block_tables), max_blocks_per_seq, batch,
+                                      max_rows, _ptr(out), _ptr(workspace), workspace_bytes, _stream(stream)),
+           "sidp_attention_shared")
 
 
 def sidp_token_logprobs_bytes(rows, vocab, top_k):

@@ -245,6 +245,17 @@ struct AttnRowsCall {
 size_t attn_rows_ws_bytes(int batch, int max_rows, int hq, int hkv, int d, int max_seq, int num_cus);
 hipError_t launch_attention_rows(const AttnRowsCall& c, hipStream_t s);
 
+// The same over the 8-bit cache (kv8.type other than 0; kv its counts only), or where groups of sequences share their first blocks:
+// see sidp_attention_rows8 and sidp_attention_shared.
+struct AttnPartsCall : AttnRowsCall {
+  Kv8View kv8;
+  const int32_t* group_starts;  // [groups + 1]
+  const int32_t* shared_lens;   // [groups]
+  int groups;
+};
+size_t attn_parts_ws_bytes(int batch, int max_rows, int hq, int hkv, int d, int num_cus, bool groups);
+hipError_t launch_attention_parts(const AttnPartsCall& c, hipStream_t s);
+
 hipError_t launch_copy(const void* src, void* dst, size_t bytes, int grid, hipStream_t s);
 
 // Rows moved between per-replica buffers and one contiguous staging buffer:

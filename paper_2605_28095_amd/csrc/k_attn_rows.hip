@@ -36,22 +36,13 @@
 // of 8192 rows 985 and 1373, eight chunks 318 and 432. Distance from 64 bits, normal
 // keys, values and queries: 0.0022 of the norm rounded, 0.0016 in two parts, which is what
 // the result's own rounding makes.
-#include <type_traits>
-
+#include "attn_tile.h"
 #include "common.h"
 #include "internal.h"
 
 namespace sidp {
 
 namespace {
-
-constexpr float kLog2e = 1.4426950408889634f;
-constexpr int kChunk = 32;        // tokens staged at a time
-constexpr int kRing = 4;          // chunks of K, and of V, in LDS
-constexpr int kChunkBlocks = kChunk / kBlockTokens;
-constexpr float kMost = 4096.f;
-constexpr int kWaves = 4;
-constexpr int kTileRows = 32 * kWaves;  // (token, head) pairs of a tile
 
 // Items (entry, KV head) the chip holds at once: two workgroups a CU.
 constexpr int kSlotsPerCu = 2;
@@ -62,8 +53,6 @@ constexpr int kMinRun = 16, kMaxRuns = 32;
 // over 1000 32, 16: 32 / 26; of 32 rows over 4000 126, 63: 96 / 98; 1 of 200 rows over 2000 69, 16: 49 / 39; 4 of 100 rows over
 // 4000 129, 56: 82 / 80; 1 of 16 rows over 30000 939, 30: 480 / 46.
 constexpr float kCutFrom = 1.75f;
-
-typedef const __attribute__((address_space(4))) int32_t cint32_t;
 
 struct Entry {
   int b, tile;
@@ -81,7 +70,6 @@ struct Layout {
   size_t entries, cuts, recs, bytes;
 };
 
-__host__ __device__ inline int tile_tokens(int group) { return kTileRows / group; }
 // for one KV head's items
 __host__ __device__ inline int slots_of(int num_cus, int hkv) { return kSlotsPerCu * (num_cus < 1 ? 1 : num_cus) / hkv; }
 
@@ -298,45 +286,8 @@ __global__ void __launch_bounds__(64 * kPlanWaves) k_attn_rows_plan(AttnRowsCall
   }
 }
 
-__device__ __forceinline__ uint32_t keep_finite(uint32_t v) {
-  const uint32_t lo = (v & 0x7f80u) == 0x7f80u ? 0u : v & 0xffffu;
-  const uint32_t hi = (v & 0x7f800000u) == 0x7f800000u ? 0u : v & 0xffff0000u;
-  return lo | hi;
-}
-__device__ __forceinline__ bool any_not_finite(uint32_t v) {
-  return (v & 0x7f80u) == 0x7f80u || (v & 0x7f800000u) == 0x7f800000u;
-}
-// 16 bytes a lane of a block (its address the same for the wave), straight to LDS: lane l's land at dst + 16 l. once: non-temporal,
-// nothing is left in the caches. A buffer load: after a global one, which the compiler takes for a flat access, it waits for every
-// LDS read instead of the one that is needed (a prompt of 8192 rows: 1013 us, so 975).
-template <int BYTES>
-__device__ __forceinline__ void load_lds16(const char* block, uint32_t offset, char* dst, bool once) {
-  const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(block), (short)0, BYTES, 0x00020000);
-  const auto to = (__attribute__((address_space(3))) void*)dst;
-  if (once) __builtin_amdgcn_raw_ptr_buffer_load_lds(r, to, 16, offset, 0, 0, 2);
-  else __builtin_amdgcn_raw_ptr_buffer_load_lds(r, to, 16, offset, 0, 0, 0);
-}
-
-// The larger of a lane's value and its counterpart's in the other half of the wave.
-__device__ __forceinline__ float max_halves(float v) {
-  const u32x2_t r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-
 template <int D>
 __global__ void __launch_bounds__(256, 2) k_attn_rows(AttnRowsCall c, Layout lay) {
-  constexpr int KK = D / 16, DT = D / 32;
-  constexpr int kBlockBytes = kBlockTokens * D * 2;
-  constexpr int kSide = kChunkBlocks * kBlockBytes;  // K or V of a chunk
-  constexpr int kBlockWaves = D / 32;                // waves that load a block's K (and V), 16 bytes a lane
-  constexpr int kPieces = kChunkBlocks * kBlockWaves / kWaves;
-  constexpr int kGroupChunks = 64 / kChunkBlocks;    // chunks whose block ids a wave holds, one a lane
-  extern __shared__ __attribute__((aligned(16))) char smem[];  // the rings of K and of V
-  __shared__ int s_odd;          // whether an edge chunk held values that are not finite
-  __shared__ int s_first[3][D];  // and the first tokens that hold +inf, -inf and NaN, of each dim
-
-  const int t = threadIdx.x, lane = t & 63, col = lane & 31, half = lane >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const char* ws = (const char*)c.ws;
   const int hkv = c.kv.hkv, group = c.hq / hkv, tm = tile_tokens(group);
   const int item = blockIdx.x;
@@ -345,353 +296,17 @@ __global__ void __launch_bounds__(256, 2) k_attn_rows(AttnRowsCall c, Layout lay
   const int g = item % hkv;
   const int b = ep[0], tile = ep[1], c0 = ep[2] & 0xffff, c1 = c0 + (int)((uint32_t)ep[2] >> 16), rec = ep[3];
   const int seq0 = ((cint32_t*)c.row_starts)[b], seq_rows = ((cint32_t*)c.row_starts)[b + 1] - seq0;
-  const int row0 = seq0 + tile * tm;
-  const int tokens = min(tm, seq_rows - tile * tm);              // of this tile
-  const int first_pos = ((cint32_t*)c.ctx_lens)[b] + tile * tm;  // of its first row
-  // A sequence of one tile reads its keys and values once: loads that leave nothing in the caches reach more of HBM's rate (16
-  // sequences of 4 rows 69 us, 77 without), but more tiles of a sequence share what one leaves there (8192 rows 1020 us, 1054).
-  // Beside such loads there is time for P in two parts.
-  const bool one_tile = seq_rows <= tm;
-  const int kv_end = first_pos + tokens;
-  const int blocks = (kv_end + kBlockTokens - 1) / kBlockTokens;
-  const int32_t* bt = c.block_tables + (int64_t)b * c.max_blocks;
-  const float scale = kLog2e / sqrtf((float)D);
-  if (t == 0) s_odd = 0;
-  for (int i = t; i < 3 * D; i += 256) (&s_first[0][0])[i] = 0x7fffffff;
-
-  // this lane's pair, its query, and the keys it sees
-  struct Pair {
-    int at, tok, head;
-  };
-  auto pair_of = [&](int thread) {
-    const int at = (thread >> 6) * 32 + (thread & 31), tok = at / group;
-    return Pair{at, tok, at - tok * group};
-  };
-  const Pair own = pair_of(t);
-  const bool live = own.tok < tokens;  // pairs past tm * group have tok >= tm
-  const int limit = live ? first_pos + own.tok + 1 : 0;
-  bf16x8_t q[KK];
-  {
-    const uint16_t* qp = c.q + ((int64_t)(row0 + (live ? own.tok : 0)) * c.hq + g * group + (live ? own.head : 0)) * D + half * 8;
-#pragma unroll
-    for (int kk = 0; kk < KK; kk++) q[kk] = as_bf16x8(*(const u32x4_t*)(qp + kk * 16));
-  }
-  // pairs of a wave are in token order: the fewest and the most keys that its pairs see
-  const int wave_first = wave * 32 / group;
-  const bool wave_live = wave_first < tokens;
-  const int wave_least = first_pos + wave_first + 1;
-  const int wave_most = wave_live ? first_pos + min(tokens, (wave * 32 + 31) / group + 1) : 0;
-
-  f32x16_t o[DT];
-  // A score x weighs 2^(x scale + base). `most`: the largest sum of a chunk's weights that leaves base alone; negative before there
-  // is a reference, kMost from then on (and for lanes without a pair).
-  float base = 0.f, most = live ? -1.f : kMost, l = 0.f;
-#pragma unroll
-  for (int dt = 0; dt < DT; dt++)
-#pragma unroll
-    for (int r = 0; r < 16; r++) o[dt][r] = 0.f;
-
-  // Places in the cache (in blocks of one KV head) of 32 chunks' blocks, one a
-  // lane, and the ids of the 32 behind them (loaded a group ahead: a wait for an id
-  // would wait for the chunks in flight too). A block outside the cache is read as
-  // block 0, one past the last block as the last.
-  bool bad = false;
-  auto load_ids = [&](int chunk) { return bt[min(chunk * kChunkBlocks + lane, blocks - 1)]; };
-  const int place0 = c.region * c.kv.nblk;
-  auto places = [&](int id) {
-    const bool ok = id >= 0 && id < c.kv.nblk;
-    bad |= !ok;
-    return (place0 + (ok ? id : 0)) * hkv + g;
-  };
-  int at_k = places(load_ids(c0)), ids_next = load_ids(c0 + kGroupChunks), at_v = at_k;  // V is fetched two chunks later
-  const int blk_wave = wave / kBlockWaves, in_block = wave % kBlockWaves;
-  // K blocks go to LDS as they are; V blocks as [token / 8][d][token % 8], so that 32 dims' pieces are contiguous
-  const uint32_t k_src = (in_block * 64 + lane) * 16;
-  const uint32_t v_src = (in_block % (kBlockWaves / 2) * 64 + lane) * 32 + in_block / (kBlockWaves / 2) * 16;
-  char* const mine = smem + blk_wave * kBlockBytes + in_block * 1024;  // this wave's first piece of a chunk
-  auto fetch = [&](int n, int at, const void* cache, uint32_t src, char* to, bool once) {  // n: chunk counted from c0
-#pragma unroll
-    for (int j = 0; j < kPieces; j++) {
-      const int from = j * (kWaves / kBlockWaves);
-      const int place = __builtin_amdgcn_readlane(at, n % kGroupChunks * kChunkBlocks + from + blk_wave);
-      load_lds16<kBlockBytes>((const char*)cache + (int64_t)place * kBlockBytes, src, to + from * kBlockBytes, once);
+  const int tokens = min(tm, seq_rows - tile * tm);
+  const int first_pos = ((cint32_t*)c.ctx_lens)[b] + tile * tm;
+  const AttnTile<true> x = {b, seq0 + tile * tm, tokens, first_pos, first_pos + tokens, c0, c1, g, seq_rows <= tm};
+  attn_tile<D, 0>(c, x, [&](const AttnOut<D>& out) {
+    if (rec < 0) {
+      out.rows(c.out);
+    } else {
+      float* r = (float*)((char*)c.ws + lay.recs) + ((int64_t)rec * hkv + g) * lay.rec_rows * (D + 2);
+      out.record(r + out.at * D, r + (int64_t)lay.rec_rows * D + 2 * out.at);
     }
-  };
-  auto fetch_k = [&](int n, int slot, bool once) {
-    if (n > 0 && n % kGroupChunks == 0) {
-      at_k = places(ids_next);
-      ids_next = load_ids(c0 + n + kGroupChunks);
-    }
-    fetch(n, at_k, c.kv.k, k_src, mine + slot * kSide, once);
-  };
-  auto fetch_v = [&](int n, int slot, bool once) {
-    if (n % kGroupChunks == 0) at_v = at_k;
-    fetch(n, at_v, c.kv.v, v_src, mine + (kRing + slot) * kSide, once);
-  };
-  // Waits for the other waves, with no LDS operation of this one under way: what it read they may load over, what it wrote they
-  // may change.
-  auto meet = [&] {
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-  };
-  // Waits until this wave's loads but the last 4 * kPieces have landed (all, with `all`), then for the other waves.
-  auto landed = [&](bool all) {
-    if (all) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    else asm volatile("s_waitcnt vmcnt(%0)" ::"n"(4 * kPieces) : "memory");
-    meet();
-  };
-  // The V of an edge chunk (one that the tile's first row does not see whole), landed. Tokens past kv_end become zeros (anything
-  // may stand there). So do values that are not finite, for 0 * inf would reach the rows that do not see them: they are added to
-  // the others at the end, where an inf or a NaN is an inf or a NaN whenever it came.
-  auto mend = [&](int ch) {
-    if ((ch + 1) * kChunk <= first_pos + 1) return;
-    int t = threadIdx.x;
-    asm volatile("" : "+v"(t));  // the addresses are made here rather than kept: no register is left for them
-    char* vb = smem + (kRing + (ch - c0) % kRing) * kSide;
-#pragma unroll 1
-    for (int i = t; i < kSide / 16; i += 256) {
-      const int t0 = ch * kChunk + i / (2 * D) * kBlockTokens + i / D % 2 * 8;
-      u32x4_t v = *(const u32x4_t*)(vb + i * 16);
-#pragma unroll
-      for (int k = 0; k < 4; k++) {
-        if (t0 + 2 * k >= kv_end) v[k] = 0;
-        else if (t0 + 2 * k + 1 >= kv_end) v[k] &= 0xffffu;
-      }
-      if (any_not_finite(v[0]) || any_not_finite(v[1]) || any_not_finite(v[2]) || any_not_finite(v[3])) {
-        s_odd = 1;
-#pragma unroll 1
-        for (int k = 0; k < 8; k++) {
-          const uint32_t h = (k & 4 ? (k & 2 ? v[3] : v[2]) : (k & 2 ? v[1] : v[0])) >> 16 * (k & 1) & 0xffffu;
-          if ((h & 0x7f80u) == 0x7f80u) atomicMin(&s_first[h == 0x7f80u ? 0 : h == 0xff80u ? 1 : 2][i % D], t0 + k);
-        }
-#pragma unroll
-        for (int k = 0; k < 4; k++) v[k] = keep_finite(v[k]);
-      }
-      *(u32x4_t*)(vb + i * 16) = v;
-    }
-    meet();
-  };
-
-  // K: the token of S^T's row m is m with bits 2 and 3 exchanged
-  const int ktok = (col & 3) | ((col >> 2) & 1) << 3 | ((col >> 3) & 1) << 2;
-  const uint32_t k_lane = (col >> 4) * kBlockBytes + (half * 16 + ktok) * 16;
-  const uint32_t v_lane = half * (D * 16) + col * 16;
-  // Register r: token 16 (r / 8) + 8 half + r % 8 of the chunk.
-  auto mask = [&](int ch, f32x16_t& s) {
-    if ((ch + 1) * kChunk > wave_least) {
-#pragma unroll
-      for (int r = 0; r < 16; r++) s[r] = ch * kChunk + 16 * (r / 8) + 8 * half + r % 8 < limit ? s[r] : -INFINITY;
-    }
-  };
-  // Eight weights as bf16: rounded, or cut (p[k]) and what the cut left (p[2 + k]). The second part gets 2^-23 of the weight more,
-  // so that it is above zero where the weight is: an infinite value stays one in both products.
-  auto to_bf16 = [&](auto parts, const float* e, bf16x8_t (&p)[4], int k) {
-    uint32_t hi[4], lo[4];
-#pragma unroll
-    for (int i = 0; i < 4; i++) {
-      if (decltype(parts)::value) {
-        const uint32_t a = __float_as_uint(e[2 * i]), b = __float_as_uint(e[2 * i + 1]);
-        hi[i] = __builtin_amdgcn_perm(b, a, 0x07060302u);  // the upper halves
-        lo[i] = pack_bf2(fmaf(e[2 * i], 1.f + 0x1p-23f, -__uint_as_float(a & 0xffff0000u)),
-                         fmaf(e[2 * i + 1], 1.f + 0x1p-23f, -__uint_as_float(b & 0xffff0000u)));
-      } else {
-        hi[i] = pack_bf2(e[2 * i], e[2 * i + 1]);
-      }
-    }
-    p[k] = as_bf16x8(u32x4_t{hi[0], hi[1], hi[2], hi[3]});
-    if (decltype(parts)::value) p[2 + k] = as_bf16x8(u32x4_t{lo[0], lo[1], lo[2], lo[3]});
-  };
-  // Where a pair's weights of a chunk have grown too large for its reference (or it has none): the reference moves to the chunk's
-  // largest score, the sums with it, and the weights are made again.
-  auto weigh = [&](auto parts, const f32x16_t& s, bf16x8_t (&p)[4], float sum) {
-    if (__any(sum > most)) {
-      float cm = s[0];
-#pragma unroll
-      for (int r = 1; r < 16; r++) cm = fmaxf(cm, s[r]);
-      cm = max_halves(cm) * scale;
-      const float old = most < 0.f ? -INFINITY : -base, now = fmaxf(old, cm);
-      if (now > -INFINITY) {
-        const float alpha = __builtin_amdgcn_exp2f(old - now);
-        base = -now;
-        most = kMost;
-        l *= alpha;
-#pragma unroll
-        for (int dt = 0; dt < DT; dt++)
-#pragma unroll
-          for (int r = 0; r < 16; r++) o[dt][r] *= alpha;
-      }
-      sum = 0.f;
-#pragma unroll
-      for (int k = 0; k < 2; k++) {
-        float e[8];
-#pragma unroll
-        for (int r = 0; r < 8; r++) {
-          e[r] = __builtin_amdgcn_exp2f(fmaf(s[8 * k + r], scale, base));
-          sum += e[r];
-        }
-        to_bf16(parts, e, p, k);
-      }
-    }
-    l += sum;
-  };
-  auto add = [&](auto parts, bf16x8_t v, const bf16x8_t (&p)[4], int k, f32x16_t& o) {
-    o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p[k], o, 0, 0, 0);
-    if (decltype(parts)::value) o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p[2 + k], o, 0, 0, 0);
-  };
-  auto add_values = [&](auto parts, int slot, const bf16x8_t (&p)[4]) {
-    const char* vb = smem + (kRing + slot) * kSide + v_lane;
-#pragma unroll
-    for (int k = 0; k < 2; k++)
-#pragma unroll
-      for (int dt = 0; dt < DT; dt++) add(parts, as_bf16x8(*(const u32x4_t*)(vb + k * kBlockBytes + dt * 512)), p, k, o[dt]);
-  };
-  // Chunk ch's weights on the vector units, while the matrix units add chunk ch - 1's values (not with `first`) and make chunk
-  // ch + 1's scores. Products take turns between the two, each with its share of the weights' arithmetic behind it, and fragments
-  // are read kAhead products ahead. (Behind the last chunk the scores are of whatever lies there, and nobody's.)
-  auto products = [&](auto first, auto parts, int slot, f32x16_t& s, f32x16_t& s_next, bf16x8_t (&p_last)[4], bf16x8_t (&p)[4]) {
-    constexpr bool kFirst = decltype(first)::value;
-    constexpr int kProducts = KK + (kFirst ? 0 : 2 * DT), kShare = 16 / kProducts, kAhead = 3;
-    const char* kb = smem + (slot + 1) % kRing * kSide + k_lane;
-    const char* vb = smem + (kRing + (slot + kRing - 1) % kRing) * kSide + v_lane;
-    u32x4_t frag[kAhead + 1];
-    auto read = [&](int i) {
-      const char* from = kFirst ? kb + i * 512 : i % 2 ? kb + i / 2 * 512 : vb + i / 2 / DT * kBlockBytes + i / 2 % DT * 512;
-      frag[i % (kAhead + 1)] = *(const u32x4_t*)from;
-    };
-    float sum = 0.f, e[16];
-#pragma unroll
-    for (int r = 0; r < 16; r++) s_next[r] = 0.f;
-    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int i = 0; i < kAhead; i++) read(i);
-#pragma unroll
-    for (int i = 0; i < kProducts; i++) {
-      __builtin_amdgcn_sched_barrier(0);
-      if (i + kAhead < kProducts) read(i + kAhead);
-      const bf16x8_t f = as_bf16x8(frag[i % (kAhead + 1)]);
-      if (kFirst || i % 2) s_next = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, q[kFirst ? i : i / 2], s_next, 0, 0, 0);
-      else add(parts, f, p_last, i / 2 / DT, o[i / 2 % DT]);
-#pragma unroll
-      for (int r = i * kShare; r < (i + 1) * kShare; r++) {
-        e[r] = __builtin_amdgcn_exp2f(fmaf(s[r], scale, base));
-        if (r > 0) sum += e[r - 1];  // a step late: nothing waits for the exponential
-        if (r % 8 == 7) to_bf16(parts, e + r - 7, p, r / 8);
-      }
-    }
-    __builtin_amdgcn_sched_barrier(0);
-    weigh(parts, s, p, sum + e[15]);
-  };
-  // A turn for chunk c0 + n: at its start V(n - 1) and K(n + 1) have landed, and V(n + 2) and K(n + 4) are fetched into the places
-  // of V(n - 2) and K(n), three turns before their use.
-  auto turn = [&](auto first, auto single, int n, f32x16_t& s, f32x16_t& s_next, bf16x8_t (&p_last)[4], bf16x8_t (&p)[4]) {
-    constexpr bool kFirst = decltype(first)::value, once = decltype(single)::value;
-    const int ch = c0 + n, slot = n % kRing;
-    if (ch + 2 < c1) fetch_v(n + 2, (n + 2) % kRing, once);
-    if (ch + 4 < c1) fetch_k(n + 4, slot, once);
-    if (ch * kChunk < wave_most) {
-      mask(ch, s);
-      products(first, single, slot, s, s_next, p_last, p);
-    } else if (!kFirst && (ch - 1) * kChunk < wave_most) {
-      add_values(single, (n + kRing - 1) % kRing, p_last);
-    }
-    landed(ch + 4 >= c1);
-    mend(ch);
-  };
-  // A run of chunks. single: of a sequence of one tile.
-  auto chunks = [&](auto single) {
-    constexpr bool once = decltype(single)::value;
-    f32x16_t sa, sb;
-    bf16x8_t pa[4], pb[4];
-    const int n_end = c1 - c0;
-    fetch_k(0, 0, once);
-    if (1 < n_end) fetch_k(1, 1, once);
-    fetch_v(0, 0, once);
-    if (2 < n_end) fetch_k(2, 2, once);
-    if (1 < n_end) fetch_v(1, 1, once);
-    if (3 < n_end) fetch_k(3, 3, once);
-    landed(4 > n_end);
-    if (c0 * kChunk < wave_most) {
-      const char* kb = smem + k_lane;
-#pragma unroll
-      for (int r = 0; r < 16; r++) sa[r] = 0.f;
-#pragma unroll
-      for (int kk = 0; kk < KK; kk++)
-        sa = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(*(const u32x4_t*)(kb + kk * 512)), q[kk], sa, 0, 0, 0);
-    }
-    meet();  // K(0) is read
-    turn(std::true_type{}, single, 0, sa, sb, pb, pa);
-    int n = 1;
-    {
-      // Turns that every row of the tile sees whole and that have chunks to fetch: the same without the questions, four at a time
-      // so that their places in the rings are constants.
-      auto plain = [&](auto slot, f32x16_t& s, f32x16_t& s_next, bf16x8_t (&p_last)[4], bf16x8_t (&p)[4]) {
-        constexpr int kSlot = decltype(slot)::value;
-        fetch_v(n + 2, (kSlot + 2) % kRing, once);
-        fetch_k(n + 4, kSlot, once);
-        if (wave_live) products(std::false_type{}, single, kSlot, s, s_next, p_last, p);
-        landed(false);
-        n++;
-      };
-      const int plain_end = min(n_end - 4, (first_pos + 1) / kChunk - c0);
-      while (n + 3 < plain_end) {
-        plain(std::integral_constant<int, 1>{}, sb, sa, pa, pb);
-        plain(std::integral_constant<int, 2>{}, sa, sb, pb, pa);
-        plain(std::integral_constant<int, 3>{}, sb, sa, pa, pb);
-        plain(std::integral_constant<int, 0>{}, sa, sb, pb, pa);
-      }
-    }
-    for (; n < n_end; n += 2) {
-      turn(std::false_type{}, single, n, sb, sa, pa, pb);
-      if (n + 1 < n_end) turn(std::false_type{}, single, n + 1, sa, sb, pb, pa);
-    }
-    if ((c1 - 1) * kChunk < wave_most) {
-      if (n_end & 1) add_values(single, (n_end - 1) % kRing, pa);
-      else add_values(single, (n_end - 1) % kRing, pb);
-    }
-  };
-  if (one_tile) chunks(std::true_type{});
-  else chunks(std::false_type{});
-  if (bad) atomicOr(c.err, SIDP_DEVERR_BLOCK);
-
-  // Register r of O^T's tile dt is dim 32 dt + 8 (r / 4) + 4 half + r % 4.
-  if (s_odd) {
-#pragma unroll
-    for (int dt = 0; dt < DT; dt++)
-#pragma unroll
-      for (int r = 0; r < 16; r++) {
-        const int d = 32 * dt + 8 * (r / 4) + 4 * half + r % 4;
-        if (s_first[0][d] < limit) o[dt][r] += INFINITY;
-        if (s_first[1][d] < limit) o[dt][r] -= INFINITY;
-        if (s_first[2][d] < limit) o[dt][r] = NAN;
-      }
-  }
-  const float sum = l + __shfl_xor(l, 32, 64);
-  int late = threadIdx.x;
-  asm volatile("" : "+v"(late));  // made again here rather than kept
-  const Pair out = pair_of(late);
-  const int from = (late >> 5 & 1) * 4;  // the lane's first dim
-  if (out.tok >= tokens) return;
-  const int64_t out_row = (int64_t)(row0 + out.tok) * c.hq + g * group + out.head;
-  if (rec < 0) {
-    const float inv = 1.f / sum;
-    uint16_t* op = c.out + out_row * D + from;
-#pragma unroll
-    for (int dt = 0; dt < DT; dt++)
-#pragma unroll
-      for (int i = 0; i < 4; i++)
-        *(u32x2_t*)(op + dt * 32 + i * 8) = u32x2_t{pack_bf2(o[dt][4 * i] * inv, o[dt][4 * i + 1] * inv),
-                                                    pack_bf2(o[dt][4 * i + 2] * inv, o[dt][4 * i + 3] * inv)};
-  } else {
-    float* r = (float*)((char*)c.ws + lay.recs) + ((int64_t)rec * hkv + g) * lay.rec_rows * (D + 2);
-#pragma unroll
-    for (int dt = 0; dt < DT; dt++)
-#pragma unroll
-      for (int i = 0; i < 4; i++)
-        *(f32x4_t*)(r + out.at * D + dt * 32 + i * 8 + from) =
-            f32x4_t{o[dt][4 * i], o[dt][4 * i + 1], o[dt][4 * i + 2], o[dt][4 * i + 3]};
-    if (from == 0) *(float2*)(r + (int64_t)lay.rec_rows * D + 2 * out.at) = make_float2(most < 0.f ? -INFINITY : -base, sum);
-  }
+  });
 }
 
 // Joins a cut tile's records in run order: four dims a thread, 1024 / D pairs of one (cut tile, KV head) a workgroup, the records
@@ -748,7 +363,7 @@ hipError_t launch_d(const AttnRowsCall& c, hipStream_t s) {
   const Layout lay = layout_of(c.batch, c.max_rows, c.hq, c.kv.hkv, D, c.max_seq, c.num_cus);
   const int waves = std::min(kPlanWaves, (std::max(c.batch, lay.tiles_cap) + 63) / 64);
   k_attn_rows_plan<<<1, 64 * waves, (3 * (size_t)c.batch + 1) * sizeof(int32_t), s>>>(c, lay);
-  const size_t lds = 2 * kRing * (size_t)kChunk * D * 2;
+  const size_t lds = tile_lds<D, 0>();
   if (lds > 32 * 1024) {
     const hipError_t e = hipFuncSetAttribute((const void*)k_attn_rows<D>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     if (e != hipSuccess) return e;

@@ -1408,38 +1408,107 @@ size_t sidp_attention_rows_bytes(const sidp_handle* h, int32_t batch, int32_t ma
   return attn_rows_ws_bytes(batch, max_rows, c.num_q_heads, c.num_kv_heads, c.head_dim, c.max_seq_len, h->num_cus);
 }
 
-int sidp_attention_rows(sidp_handle* h, const void* q, int32_t region, const int32_t* row_starts,
-                        const int32_t* ctx_lens, const int32_t* block_tables, int32_t max_blocks_per_seq, int32_t batch,
-                        int32_t max_rows, void* out, void* workspace, size_t workspace_bytes, void* stream) {
-  if (!h || !attention_rows_ok(batch, max_rows) || max_blocks_per_seq < 1) return SIDP_EINVAL;
-  if (max_blocks_per_seq > (1 << 20) / kBlockTokens) return SIDP_EINVAL;
+// Checks the arguments that the calls of several new tokens share, and fills in what does not depend on the cache. `rows` is 0 where
+// there is nothing to do. regions: of the call's cache, 0 if there is none.
+static int attention_rows_call(sidp_handle* h, const void* q, int32_t region, int regions, const int32_t* row_starts,
+                               const int32_t* ctx_lens, const int32_t* block_tables, int32_t max_blocks_per_seq, int32_t batch,
+                               int32_t max_rows, void* out, void* workspace, size_t workspace_bytes, size_t needed,
+                               AttnRowsCall* a) {
+  if (max_blocks_per_seq < 1 || max_blocks_per_seq > (1 << 20) / kBlockTokens) return SIDP_EINVAL;
   if (h->poisoned) return SIDP_ESTATE;
-  if (!h->k_cache) return SIDP_ESTATE;
-  if (region < 0 || region >= h->regions) return SIDP_EINVAL;
+  if (regions == 0) return SIDP_ESTATE;
+  if (region < 0 || region >= regions) return SIDP_EINVAL;
+  a->max_rows = max_rows;
   if (max_rows == 0) return SIDP_OK;
   if (!q || !row_starts || !ctx_lens || !block_tables || !out || !workspace) return SIDP_EINVAL;
   if (((uintptr_t)q | (uintptr_t)out | (uintptr_t)workspace) % 16) return SIDP_EINVAL;
-  if (workspace_bytes < sidp_attention_rows_bytes(h, batch, max_rows)) return SIDP_EINVAL;
+  if (needed == 0 || workspace_bytes < needed) return SIDP_EINVAL;
+  a->q = (const uint16_t*)q;
+  a->row_starts = row_starts;
+  a->ctx_lens = ctx_lens;
+  a->block_tables = block_tables;
+  a->max_blocks = max_blocks_per_seq;
+  a->batch = batch;
+  a->max_seq = h->cfg.max_seq_len;
+  a->hq = h->cfg.num_q_heads;
+  a->kv = kv_view(h);
+  a->region = region;
+  a->out = (uint16_t*)out;
+  a->ws = workspace;
+  a->err = h->err;
+  a->num_cus = h->num_cus;
+  return SIDP_OK;
+}
+
+int sidp_attention_rows(sidp_handle* h, const void* q, int32_t region, const int32_t* row_starts,
+                        const int32_t* ctx_lens, const int32_t* block_tables, int32_t max_blocks_per_seq, int32_t batch,
+                        int32_t max_rows, void* out, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!h || !attention_rows_ok(batch, max_rows)) return SIDP_EINVAL;
   AttnRowsCall a;
-  a.q = (const uint16_t*)q;
-  a.row_starts = row_starts;
-  a.ctx_lens = ctx_lens;
-  a.block_tables = block_tables;
-  a.max_blocks = max_blocks_per_seq;
-  a.batch = batch;
-  a.max_rows = max_rows;
-  a.max_seq = h->cfg.max_seq_len;
-  a.hq = h->cfg.num_q_heads;
-  a.kv = kv_view(h);
-  a.region = region;
-  a.out = (uint16_t*)out;
-  a.ws = workspace;
-  a.err = h->err;
-  a.num_cus = h->num_cus;
+  const int bad = attention_rows_call(h, q, region, h->k_cache ? h->regions : 0, row_starts, ctx_lens, block_tables, max_blocks_per_seq,
+                                      batch, max_rows, out, workspace, workspace_bytes, sidp_attention_rows_bytes(h, batch, max_rows), &a);
+  if (bad != SIDP_OK || a.max_rows == 0) return bad;
   const OnDevice on(h->device);
   HIPCHK(h, on.err);
   HIPCHK(h, launch_attention_rows(a, (hipStream_t)stream));
   return SIDP_OK;
+}
+
+static size_t attention_parts_bytes(const sidp_handle* h, int32_t batch, int32_t max_rows, bool groups) {
+  if (!h || !attention_rows_ok(batch, max_rows) || max_rows < 1) return 0;
+  const sidp_config& c = h->cfg;
+  return attn_parts_ws_bytes(batch, max_rows, c.num_q_heads, c.num_kv_heads, c.head_dim, h->num_cus, groups);
+}
+
+size_t sidp_attention_rows8_bytes(const sidp_handle* h, int32_t batch, int32_t max_rows) {
+  return attention_parts_bytes(h, batch, max_rows, false);
+}
+
+size_t sidp_attention_shared_bytes(const sidp_handle* h, int32_t cache, int32_t batch, int32_t max_rows) {
+  if (cache != SIDP_CACHE_BF16 && cache != SIDP_CACHE_8BIT) return 0;
+  return attention_parts_bytes(h, batch, max_rows, true);
+}
+
+static int attention_parts(sidp_handle* h, int32_t cache, const void* q, int32_t region, const int32_t* group_starts,
+                           const int32_t* shared_lens, int32_t groups, const int32_t* row_starts, const int32_t* ctx_lens,
+                           const int32_t* block_tables, int32_t max_blocks_per_seq, int32_t batch, int32_t max_rows, void* out,
+                           void* workspace, size_t workspace_bytes, size_t needed, void* stream) {
+  AttnPartsCall a;
+  const bool bits8 = cache == SIDP_CACHE_8BIT;
+  const int regions = bits8 ? (h->kv8.k ? h->kv8.regions : 0) : (h->k_cache ? h->regions : 0);
+  const int bad = attention_rows_call(h, q, region, regions, row_starts, ctx_lens, block_tables, max_blocks_per_seq, batch, max_rows, out,
+                                      workspace, workspace_bytes, needed, &a);
+  if (bad != SIDP_OK || a.max_rows == 0) return bad;
+  a.kv8 = Kv8View{};
+  if (bits8) {
+    a.kv8 = h->kv8;
+    a.kv.nblk = h->kv8.nblk;
+  }
+  a.group_starts = group_starts;
+  a.shared_lens = shared_lens;
+  a.groups = groups;
+  const OnDevice on(h->device);
+  HIPCHK(h, on.err);
+  HIPCHK(h, launch_attention_parts(a, (hipStream_t)stream));
+  return SIDP_OK;
+}
+
+int sidp_attention_rows8(sidp_handle* h, const void* q, int32_t region, const int32_t* row_starts, const int32_t* ctx_lens,
+                         const int32_t* block_tables, int32_t max_blocks_per_seq, int32_t batch, int32_t max_rows, void* out,
+                         void* workspace, size_t workspace_bytes, void* stream) {
+  if (!h || !attention_rows_ok(batch, max_rows)) return SIDP_EINVAL;
+  return attention_parts(h, SIDP_CACHE_8BIT, q, region, nullptr, nullptr, 0, row_starts, ctx_lens, block_tables, max_blocks_per_seq, batch,
+                         max_rows, out, workspace, workspace_bytes, sidp_attention_rows8_bytes(h, batch, max_rows), stream);
+}
+
+int sidp_attention_shared(sidp_handle* h, int32_t cache, const void* q, int32_t region, const int32_t* group_starts,
+                          const int32_t* shared_lens, int32_t groups, const int32_t* row_starts, const int32_t* ctx_lens,
+                          const int32_t* block_tables, int32_t max_blocks_per_seq, int32_t batch, int32_t max_rows, void* out,
+                          void* workspace, size_t workspace_bytes, void* stream) {
+  if (!h || !attention_rows_ok(batch, max_rows) || (cache != SIDP_CACHE_BF16 && cache != SIDP_CACHE_8BIT)) return SIDP_EINVAL;
+  if (groups < 0 || groups > batch || (groups > 0 && (!group_starts || !shared_lens))) return SIDP_EINVAL;
+  return attention_parts(h, cache, q, region, group_starts, shared_lens, groups, row_starts, ctx_lens, block_tables, max_blocks_per_seq,
+                         batch, max_rows, out, workspace, workspace_bytes, sidp_attention_shared_bytes(h, cache, batch, max_rows), stream);
 }
 
 // ---------------------------------------------------------------- answers
