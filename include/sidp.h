@@ -713,6 +713,40 @@ int sidp_token_logprobs(const void *logits, int32_t dtype, int32_t rows, int32_t
                         const int32_t *targets, int32_t top_k, float *logprobs, int32_t *ranks, float *entropies,
                         int32_t *top_ids, float *top_logprobs, void *workspace, size_t workspace_bytes, void *stream);
 
+/* A token of each row of logits (the output projection of sidp_linear, say), drawn from a
+ * given random number, on the current device. Every row has settings of its own; an
+ * array that is NULL leaves its setting out.
+ *  logits, dtype, rows, vocab, row_stride  as in sidp_token_logprobs; rows at most
+ *                SIDP_SAMPLE_MAX_ROWS.
+ *  temperatures  device fp32 [rows]: T >= 0; 0 takes the most likely token (NULL: 1).
+ *  top_ks        device int32 [rows]: k, off at 0 and below and from vocab on.
+ *  top_ps        device fp32 [rows]: p >= 0, off from 1 on.
+ *  min_ps        device fp32 [rows]: 0 (off) to 1.
+ *  uniforms      device fp32 [rows]: u, 0 <= u < 1.
+ *  tokens        device int32 [rows].
+ *  logprobs      device fp32 [rows] or NULL: the token's log probability among those it
+ *                was drawn from.
+ *  kept          device int32 [rows] or NULL: how many those were.
+ * Tokens are in order of their logits, of equal ones the lowest first; w_i = exp((x_i -
+ * max x) / T). Top-k keeps the first k tokens; top-p, of those, the ones with less than
+ * p times the k tokens' weight in front of them, the first one always; min-p the ones
+ * with w_i >= min_p. Drawn is the first token, in order, at which the running weight of
+ * what all three keep exceeds u times their weight together. Weights are held to 2^-44
+ * of the largest, in whole numbers, so that a row's draw does not depend on the call's
+ * other rows nor on the machine. -inf is a masked token (never drawn, never counted). A
+ * row without a distribution (a NaN or +inf, or nothing but -inf) or with a setting that
+ * is none (NaN, or outside what stands above) gets token -1, NaN and 0.
+ *  workspace     device, 16-byte aligned, sidp_sample_tokens_bytes of the same sizes;
+ *                nothing in it outlives the call, but calls that overlap in time may not
+ *                share one. */
+#define SIDP_SAMPLE_MAX_ROWS (1 << 16)
+/* 0 for sizes that sidp_sample_tokens refuses. */
+size_t sidp_sample_tokens_bytes(int32_t rows, int32_t vocab);
+int sidp_sample_tokens(const void *logits, int32_t dtype, int32_t rows, int32_t vocab, int64_t row_stride,
+                       const float *temperatures, const int32_t *top_ks, const float *top_ps, const float *min_ps,
+                       const float *uniforms, int32_t *tokens, float *logprobs, int32_t *kept, void *workspace,
+                       size_t workspace_bytes, void *stream);
+
 /* Device-to-device copy by the library's copy kernel (the slot-fill engine),
  * using `grid` workgroups (0 = default). src, dst 16-byte aligned. */
 int sidp_copy(const void *src, void *dst, size_t bytes, int32_t grid, void *stream);

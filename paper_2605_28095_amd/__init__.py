@@ -58,6 +58,7 @@ EXPORTED = [
     "sidp_attention_rows_bytes", "sidp_attention_rows", "sidp_token_logprobs_bytes", "sidp_token_logprobs",
     "sidp_kv8_region_bytes", "sidp_kv8_scale_bytes", "sidp_kv8_attach", "sidp_rope_append_rows8", "sidp_kv8_read",
     "sidp_attention_rows8_bytes", "sidp_attention_rows8", "sidp_attention_shared_bytes", "sidp_attention_shared",
+    "sidp_sample_tokens_bytes", "sidp_sample_tokens",
 ]
 
 SIDP_CAS_MAX_REPLICAS = 16
@@ -75,6 +76,7 @@ SIDP_KV_INT8 = 2
 SIDP_CACHE_BF16 = 0
 SIDP_CACHE_8BIT = 1
 SIDP_MAX_ROWS = 1 << 20
+SIDP_SAMPLE_MAX_ROWS = 1 << 16
 
 
 class SidpError(RuntimeError):
@@ -144,6 +146,8 @@ _sigs = {
     "sidp_attention_rows8": (ctypes.c_int, [_P, _P, _I, _P, _P, _P, _I, _I, _I, _P, _P, _Z, _P]),
     "sidp_attention_shared_bytes": (_Z, [_P, _I, _I, _I]),
     "sidp_attention_shared": (ctypes.c_int, [_P, _I, _P, _I, _P, _P, _I, _P, _P, _P, _I, _I, _I, _P, _P, _Z, _P]),
+    "sidp_sample_tokens_bytes": (_Z, [_I, _I]),
+    "sidp_sample_tokens": (ctypes.c_int, [_P, _I, _I, _I, ctypes.c_int64, _P, _P, _P, _P, _P, _P, _P, _P, _P, _Z, _P]),
     "sidp_kv8_region_bytes": (_Z, [ctypes.POINTER(sidp_config), _I]),
     "sidp_kv8_scale_bytes": (_Z, [ctypes.POINTER(sidp_config), _I]),
     "sidp_kv8_attach": (ctypes.c_int, [_P, _I, _P, _P, _P, _I, _I]),
@@ -534,6 +538,17 @@ def sidp_token_logprobs(logits, dtype, rows, vocab, row_stride, targets, top_k, 
     _check(_lib.sidp_token_logprobs(_ptr(logits), dtype, rows, vocab, row_stride, _ptr(targets), top_k, _ptr(logprobs),
                                     _ptr(ranks), _ptr(entropies), _ptr(top_ids), _ptr(top_logprobs), _ptr(workspace),
                                     workspace_bytes, _stream(stream)), "sidp_token_logprobs")
+
+
+def sidp_sample_tokens_bytes(rows, vocab):
+    return _lib.sidp_sample_tokens_bytes(rows, vocab)
+
+
+def sidp_sample_tokens(logits, dtype, rows, vocab, row_stride, temperatures, top_ks, top_ps, min_ps, uniforms, tokens,
+                       logprobs, kept, workspace, workspace_bytes, stream=None):
+    _check(_lib.sidp_sample_tokens(_ptr(logits), dtype, rows, vocab, row_stride, _ptr(temperatures), _ptr(top_ks),
+                                   _ptr(top_ps), _ptr(min_ps), _ptr(uniforms), _ptr(tokens), _ptr(logprobs), _ptr(kept),
+                                   _ptr(workspace), workspace_bytes, _stream(stream)), "sidp_sample_tokens")
 
 
 def sidp_copy(src, dst, nbytes, grid=0, stream=None):

@@ -193,6 +193,24 @@ struct LogprobCall {
 size_t logprob_ws_bytes(int rows, int vocab, int top);
 hipError_t launch_logprobs(LogprobCall c, hipStream_t s);
 
+struct SampleCall {
+  const void* logits;
+  bool f32;
+  int rows, vocab;
+  int64_t stride;
+  const float* temperatures;
+  const int32_t* top_ks;
+  const float* top_ps;
+  const float* min_ps;
+  const float* uniforms;
+  int32_t* tokens;
+  float* logprobs;
+  int32_t* kept;
+  void* ws;
+};
+size_t sample_ws_bytes(int rows, int vocab);
+hipError_t launch_sample(const SampleCall& c, hipStream_t s);
+
 struct AttnCall {
   const uint16_t* q;  // [B][Hq][D]
   const int32_t* positions;

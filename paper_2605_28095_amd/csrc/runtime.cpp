@@ -1550,6 +1550,29 @@ int sidp_token_logprobs(const void* logits, int32_t dtype, int32_t rows, int32_t
   return launch_logprobs(c, (hipStream_t)stream) == hipSuccess ? SIDP_OK : SIDP_EHIP;
 }
 
+static bool sample_ok(int32_t rows, int32_t vocab) {
+  return rows >= 0 && rows <= SIDP_SAMPLE_MAX_ROWS && vocab >= 1 && vocab <= SIDP_LOGPROBS_MAX_VOCAB;
+}
+
+size_t sidp_sample_tokens_bytes(int32_t rows, int32_t vocab) {
+  if (!sample_ok(rows, vocab) || rows < 1) return 0;
+  return align_up(sample_ws_bytes(rows, vocab), kAlign);
+}
+
+int sidp_sample_tokens(const void* logits, int32_t dtype, int32_t rows, int32_t vocab, int64_t row_stride,
+                       const float* temperatures, const int32_t* top_ks, const float* top_ps, const float* min_ps,
+                       const float* uniforms, int32_t* tokens, float* logprobs, int32_t* kept, void* workspace,
+                       size_t workspace_bytes, void* stream) {
+  if (!sample_ok(rows, vocab) || row_stride < vocab) return SIDP_EINVAL;
+  if (dtype != SIDP_LOGITS_BF16 && dtype != SIDP_LOGITS_F32) return SIDP_EINVAL;
+  if (rows == 0) return SIDP_OK;
+  if (!logits || (uintptr_t)logits % (dtype == SIDP_LOGITS_F32 ? 4 : 2) || !uniforms || !tokens) return SIDP_EINVAL;
+  if (!workspace || (uintptr_t)workspace % 16 || workspace_bytes < sidp_sample_tokens_bytes(rows, vocab)) return SIDP_EINVAL;
+  const SampleCall c = {logits, dtype == SIDP_LOGITS_F32, rows,     vocab,  row_stride, temperatures, top_ks,
+                        top_ps, min_ps,                   uniforms, tokens, logprobs,   kept,         workspace};
+  return launch_sample(c, (hipStream_t)stream) == hipSuccess ? SIDP_OK : SIDP_EHIP;
+}
+
 int sidp_copy(const void* src, void* dst, size_t bytes, int32_t grid, void* stream) {
   if ((!src || !dst) && bytes) return SIDP_EINVAL;
   if (((uintptr_t)src % 16) || ((uintptr_t)dst % 16) || grid < 0) return SIDP_EINVAL;
