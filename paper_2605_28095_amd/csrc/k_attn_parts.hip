@@ -13,6 +13,7 @@
 //
 // Only whole chunks of 32 tokens are shared; the rest of the prefix is read by each
 // sequence as its own. A group shares where its tiles are at most half of its sequences'.
+#include "attn_few8.h"
 #include "attn_tile.h"
 #include "common.h"
 #include "internal.h"
@@ -103,7 +104,6 @@ __global__ void __launch_bounds__(64 * kPlanWaves) k_attn_parts_plan(AttnPartsCa
   int32_t* s_seq = s_chunks + G;       // [G] the first sequence with rows
   int32_t* s_own = s_seq + G;          // [G] its sequences' tiles, and later its first record
   int32_t* s_grows = s_own + G;        // [G] rows
-  int32_t* s_row0 = s_grows + G;       // [G] first row
   char* ws = (char*)c.ws;
   int32_t* counts = (int32_t*)ws;
   Entry* entries = (Entry*)(ws + lay.entries);
@@ -167,7 +167,6 @@ __global__ void __launch_bounds__(64 * kPlanWaves) k_attn_parts_plan(AttnPartsCa
       const int row0 = c.row_starts[s_first[i]], rows = c.row_starts[s_grows[i]] - row0;
       const bool shares = s_chunks[i] / kChunk >= kLeastShared && s_own[i] > 0 && 2 * ((rows + tm - 1) / tm) <= s_own[i];
       s_chunks[i] = shares ? s_chunks[i] / kChunk : 0;
-      s_row0[i] = row0;
       s_grows[i] = shares ? rows : 0;
     }
     __syncthreads();
@@ -318,7 +317,7 @@ __global__ void __launch_bounds__(64 * kPlanWaves) k_attn_parts_plan(AttnPartsCa
     const int parts = parts_of(x);
     const bool shared = x.i < G, rec = parts > 1 || x.rec;
     const int b = shared ? s_seq[x.i] : x.i - G;
-    const int row0 = (shared ? s_row0[x.i] : c.row_starts[b]) + x.place * tm;
+    const int row0 = c.row_starts[shared ? c.group_starts[x.i] : b] + x.place * tm;
     const int end = shared ? x.chunks * kChunk : s_ctx[b] + x.place * tm + x.rows;
     const bool alone = (shared ? s_grows[x.i] : s_rows[b]) <= tm;
     // Within a step of length the order is whatever the atomics give; items write places of their own, so results do not depend on it.
@@ -334,7 +333,7 @@ __global__ void __launch_bounds__(64 * kPlanWaves) k_attn_parts_plan(AttnPartsCa
       if (i >= 0) {
         cut.grec = s_own[i];
         cut.gparts = (s_chunks[i] + run - 1) / run;
-        cut.goff = row0 - s_row0[i];
+        cut.goff = row0 - c.row_starts[c.group_starts[i]];
         cut.grows = s_grows[i];
       }
       cuts[atomicAdd(&s_cuts, 1)] = cut;
@@ -358,12 +357,31 @@ __global__ void __launch_bounds__(256, 2) k_attn_parts(AttnPartsCall c, Layout l
   const int c0 = ep[5] & 0xffff, rec = ep[6], flags = ep[7];
   const AttnTile<false> x = {ep[0], ep[1], ep[2], ep[3], ep[4], c0, c0 + (int)((uint32_t)ep[5] >> 16), item % hkv,
                              (flags & kOneTile) != 0, flags & kOwnKeys};
+  float* const recs = (float*)((char*)c.ws + lay.recs);
+  float* const sums = (float*)((char*)c.ws + lay.sums);
+  if constexpr (TYPE != 0) {
+    const int group = c.hq / hkv, pairs = x.tokens * group;
+    auto emit = [&](int tok, int head, int dim, f32x4_t o, float sum, float ref) {
+      const int at = item % hkv * group + head;
+      if (rec < 0) {
+        const float inv = 1.f / sum;
+        *(u32x2_t*)(c.out + ((int64_t)(x.row0 + tok) * c.hq + at) * D + dim) =
+            u32x2_t{pack_bf2(o[0] * inv, o[1] * inv), pack_bf2(o[2] * inv, o[3] * inv)};
+      } else {
+        const int64_t to = (int64_t)(rec + tok) * c.hq + at;
+        *(f32x4_t*)(recs + to * D + dim) = o;
+        if (dim == 0) *(float2*)(sums + to * 2) = make_float2(ref, sum);
+      }
+    };
+    if (pairs <= 16) return attn_few8<D, TYPE, 1>(c, x, 1, emit);
+    if (pairs <= 64) return attn_few8<D, TYPE, 2>(c, x, pairs <= 32 ? 1 : 2, emit);
+  }
   attn_tile<D, TYPE>(c, x, [&](const AttnOut<D>& out) {
     if (rec < 0) {
       out.rows(c.out);
     } else {
       const int64_t at = out.row + (int64_t)(rec - x.row0) * c.hq;  // the same head of the record
-      out.record((float*)((char*)c.ws + lay.recs) + at * D, (float*)((char*)c.ws + lay.sums) + at * 2);
+      out.record(recs + at * D, sums + at * 2);
     }
   });
 }
@@ -429,12 +447,13 @@ template <int D, int TYPE>
 hipError_t launch_type(const AttnPartsCall& c, hipStream_t s) {
   const Layout lay = layout_of(c.batch, c.max_rows, c.hq, c.kv.hkv, D, c.num_cus, c.groups > 0);
   const int waves = std::min(kPlanWaves, (std::max(c.batch, lay.tiles_cap + (c.groups > 0 ? lay.tiles_cap / 2 : 0)) + 63) / 64);
-  const size_t plan_lds = (4 * (size_t)c.batch + 6 * (size_t)c.groups + 1) * sizeof(int32_t);
+  const size_t plan_lds = (4 * (size_t)c.batch + 5 * (size_t)c.groups + 1) * sizeof(int32_t);
   hipError_t e = allow_lds((const void*)k_attn_parts_plan, plan_lds);
-  if (e == hipSuccess) e = allow_lds((const void*)k_attn_parts<D, TYPE>, tile_lds<D, TYPE>());
+  constexpr int lds = TYPE ? std::max(tile_lds<D, TYPE>(), few_lds<D, 2>()) : tile_lds<D, TYPE>();
+  if (e == hipSuccess) e = allow_lds((const void*)k_attn_parts<D, TYPE>, lds);
   if (e != hipSuccess) return e;
   k_attn_parts_plan<<<1, 64 * waves, plan_lds, s>>>(c, lay);
-  k_attn_parts<D, TYPE><<<(unsigned)((int64_t)lay.entries_cap * c.kv.hkv), 256, tile_lds<D, TYPE>(), s>>>(c, lay);
+  k_attn_parts<D, TYPE><<<(unsigned)((int64_t)lay.entries_cap * c.kv.hkv), 256, lds, s>>>(c, lay);
   // workgroups a cut and KV head: as many as its rows need, or as fill the chip
   const int most = (std::min(tile_tokens(c.hq / c.kv.hkv), c.max_rows) * (c.hq / c.kv.hkv) + 1024 / D - 1) / (1024 / D);
   const int z = std::max<int64_t>(1, std::min<int64_t>(most, 4 * (int64_t)c.num_cus / std::max<int64_t>(1, (int64_t)lay.cuts_cap * c.kv.hkv)));

@@ -189,25 +189,32 @@ __global__ void __launch_bounds__(256) k_kv8_read(Kv8ReadCall c) {
     }
     __syncthreads();
   }
-  // a row's 16 dims a thread
-  for (int i = t; i < TILE * (D / 16); i += 256) {
-    const int r = i / (D / 16), d16 = i % (D / 16), slot = s_slot[r];
-    if (slot < 0) continue;
-    const u32x4_t w = value ? *(const u32x4_t*)(s_x + r * kRow + d16 * 16)
-                            : *(const u32x4_t*)(c.kv8.k + place_of(slot) * (int64_t)(D * kBlockTokens) +
-                                                (d16 * kBlockTokens + slot % kBlockTokens) * 16);
-    const float scale = s_scale[r];
-    u32x4_t o[2];
+  // a row's 16 dims a thread, from LDS or from the cache
+  auto put = [&](auto from) {
+    for (int i = t; i < TILE * (D / 16); i += 256) {
+      const int r = i / (D / 16), d16 = i % (D / 16), slot = s_slot[r];
+      if (slot < 0) continue;
+      const u32x4_t w = from(r, d16, slot);
+      const float scale = s_scale[r];
+      u32x4_t o[2];
 #pragma unroll
-    for (int k = 0; k < 4; k++) {
-      float x[4];
-      kv8_values<TYPE>(w[k], x);
-      o[k / 2][k % 2 * 2] = pack_bf2(x[0] * scale, x[1] * scale);
-      o[k / 2][k % 2 * 2 + 1] = pack_bf2(x[2] * scale, x[3] * scale);
+      for (int k = 0; k < 4; k++) {
+        float x[4];
+        kv8_values<TYPE>(w[k], x);
+        o[k / 2][k % 2 * 2] = pack_bf2(x[0] * scale, x[1] * scale);
+        o[k / 2][k % 2 * 2 + 1] = pack_bf2(x[2] * scale, x[3] * scale);
+      }
+      uint16_t* to = out + ((int64_t)(row0 + r) * hkv + head) * D + d16 * 16;
+      *(u32x4_t*)to = o[0];
+      *(u32x4_t*)(to + 8) = o[1];
     }
-    uint16_t* to = out + ((int64_t)(row0 + r) * hkv + head) * D + d16 * 16;
-    *(u32x4_t*)to = o[0];
-    *(u32x4_t*)(to + 8) = o[1];
+  };
+  if (value) {
+    put([&](int r, int d16, int) { return *(const u32x4_t*)(s_x + r * kRow + d16 * 16); });
+  } else {
+    put([&](int, int d16, int slot) {
+      return *(const u32x4_t*)(c.kv8.k + place_of(slot) * (int64_t)(D * kBlockTokens) + (d16 * kBlockTokens + slot % kBlockTokens) * 16);
+    });
   }
 }
 

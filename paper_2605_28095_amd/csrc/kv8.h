@@ -48,8 +48,12 @@ __device__ __forceinline__ void kv8_values(uint32_t w, float (&x)[4]) {
     x[2] = hi[0];
     x[3] = hi[1];
   } else {
-#pragma unroll
-    for (int i = 0; i < 4; i++) x[i] = (float)(int8_t)(w >> 8 * i);
+    // A byte's sign and conversion in one instruction each. As casts they are taken apart, and the compiler extracts the bytes of all
+    // codes at hand first, past the registers.
+    asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_0" : "=v"(x[0]) : "v"(w));
+    asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_1" : "=v"(x[1]) : "v"(w));
+    asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_2" : "=v"(x[2]) : "v"(w));
+    asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_3" : "=v"(x[3]) : "v"(w));
   }
 }
 
