@@ -22,10 +22,11 @@ namespace {
 template <int D, int NT>
 constexpr int few_lds() { return kWaves * 16 * NT * (D + 4 + 2) * (int)sizeof(float); }
 
-// NT: tiles of 16 pairs of a wave. sides: 1 or 2 groups of waves, each with pairs of its own; 4 / sides waves share the keys.
+// NT: tiles of 16 pairs of a wave. sides: 1, 2 or 4 groups of waves, each with pairs of its own; 4 / sides waves share the keys.
 // emit(token, head, dim, values of dims dim .. dim + 3 not yet divided, sum, reference).
 template <int D, int TYPE, int NT, class Call, class Emit>
 __device__ __forceinline__ void attn_few8(const Call& c, const AttnTile<false>& x, int sides, const Emit& emit) {
+  constexpr bool kTwo = NT == 1;     // P in two parts
   constexpr int J = D / 64;          // loads of 16 bytes a lane of a block's K, and of its V
   constexpr int kGroupChunks = 32;   // chunks whose block ids a wave holds, two lanes each
   extern __shared__ __attribute__((aligned(16))) char smem[];
@@ -77,28 +78,35 @@ __device__ __forceinline__ void attn_few8(const Call& c, const AttnTile<false>& 
     at = places(load_ids(0));
     ids_next = load_ids(kGroupChunks);
   }
+  // Codes of kDepth chunks on their way, a chunk's K refilled as soon as its scores are made, its V as soon as its values are added.
+  // With two tiles of pairs the registers hold one chunk's: 16 x 8 rows over 4000 66 us with two, some of them spilled, 61 with one.
+  constexpr int kDepth = NT == 1 ? 2 : 1;
   struct Codes {
-    u32x4_t k[kChunkBlocks][J], v[kChunkBlocks][J];
-    f32x4_t ks[kChunkBlocks], vs[kChunkBlocks];
+    u32x4_t code[kChunkBlocks][J];
+    f32x4_t scale[kChunkBlocks];
   };
-  auto fetch = [&](int n, Codes& w) {
+  Codes kw[kDepth], vw[kDepth];
+  int at_v = at;
+  auto load = [&](auto single, int n, int places, const uint8_t* codes, const float* scales, Codes& w) {
+    constexpr bool once = decltype(single)::value;
+#pragma unroll
+    for (int b = 0; b < kChunkBlocks; b++) {
+      const int64_t place = __builtin_amdgcn_readlane(places, n % kGroupChunks * kChunkBlocks + b);
+#pragma unroll
+      for (int j = 0; j < J; j++) w.code[b][j] = load16<kBlockTokens * D>(codes + place * (kBlockTokens * D), 1024 * j + 16 * lane, once);
+      w.scale[b] = __builtin_bit_cast(f32x4_t, load16<kBlockTokens * 4>(scales + place * (2 * kBlockTokens), 16 * kg, false));
+    }
+  };
+  auto fetch_k = [&](auto single, int n, Codes& w) {
     if (n > 0 && n % kGroupChunks == 0) {
       at = places(ids_next);
       ids_next = load_ids(n + kGroupChunks);
     }
-#pragma unroll
-    for (int b = 0; b < kChunkBlocks; b++) {
-      const int64_t place = __builtin_amdgcn_readlane(at, n % kGroupChunks * kChunkBlocks + b);
-      const u32x4_t* kp = (const u32x4_t*)(c.kv8.k + place * (kBlockTokens * D)) + lane;
-      const u32x4_t* vp = (const u32x4_t*)(c.kv8.v + place * (kBlockTokens * D)) + lane;
-      const f32x4_t* sp = (const f32x4_t*)(c.kv8.scales + place * (2 * kBlockTokens)) + kg;
-#pragma unroll
-      for (int j = 0; j < J; j++) w.k[b][j] = __builtin_nontemporal_load(kp + 64 * j);
-      w.ks[b] = sp[0];
-#pragma unroll
-      for (int j = 0; j < J; j++) w.v[b][j] = __builtin_nontemporal_load(vp + 64 * j);
-      w.vs[b] = sp[kBlockTokens / 4];
-    }
+    load(single, n, at, c.kv8.k, c.kv8.scales, w);
+  };
+  auto fetch_v = [&](auto single, int n, Codes& w) {
+    if (n % kGroupChunks == 0) at_v = at;
+    load(single, n, at_v, c.kv8.v, c.kv8.scales + kBlockTokens, w);
   };
   const float scale = kLog2e / sqrtf((float)D);
   // The largest of the four lanes that hold a pair's scores.
@@ -108,7 +116,7 @@ __device__ __forceinline__ void attn_few8(const Call& c, const AttnTile<false>& 
     const u32x2_t b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
   };
-  auto chunk = [&](int n, Codes& w) {
+  auto chunk = [&](auto single, int n, Codes& wk, Codes& wv) {
     const int token0 = (first + n * turns) * kChunk;
     const bool edge = token0 + kChunk > least;
     // scores; register r of block b is token 16 b + 4 kg + r
@@ -121,33 +129,42 @@ __device__ __forceinline__ void attn_few8(const Call& c, const AttnTile<false>& 
       for (int j = 0; j < J; j++)
 #pragma unroll
         for (int h = 0; h < 2; h++) {
-          const u32x2_t lo = kv8_bf16<TYPE>(w.k[b][j][2 * h]), hi = kv8_bf16<TYPE>(w.k[b][j][2 * h + 1]);
+          const u32x2_t lo = kv8_bf16<TYPE>(wk.code[b][j][2 * h]), hi = kv8_bf16<TYPE>(wk.code[b][j][2 * h + 1]);
           const bf16x8_t k = as_bf16x8(u32x4_t{lo[0], lo[1], hi[0], hi[1]});
 #pragma unroll
           for (int nt = 0; nt < NT; nt++) s[nt][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[nt][2 * j + h], s[nt][b], 0, 0, 0);
           if (TYPE == kInt8) __builtin_amdgcn_sched_barrier(0);  // or all codes are spread out at once, past the registers
         }
     }
+    float ks[8];
+#pragma unroll
+    for (int i = 0; i < 8; i++) ks[i] = wk.scale[i / 4][i % 4] * scale;
+    if (n + kDepth < count) fetch_k(single, n + kDepth, wk);
     bf16x8_t p[NT][2];
 #pragma unroll
     for (int nt = 0; nt < NT; nt++) {
-      float y[8], e[8], sum = 0.f;
+      auto seen = [&](int i) { return token0 + i / 4 * kBlockTokens + kg * 4 + i % 4 < limit[nt]; };
+      float e[8], sum = 0.f;
+      auto weigh = [&] {
+        sum = 0.f;
 #pragma unroll
-      for (int i = 0; i < 8; i++) y[i] = s[nt][i / 4][i % 4] * (w.ks[i / 4][i % 4] * scale);
-      if (edge) {
+        for (int i = 0; i < 8; i++) e[i] = fmaf(s[nt][i / 4][i % 4], ks[i], base[nt]);
+        if (edge) {
 #pragma unroll
-        for (int i = 0; i < 8; i++) y[i] = token0 + i / 4 * kBlockTokens + kg * 4 + i % 4 < limit[nt] ? y[i] : -INFINITY;
-      }
+          for (int i = 0; i < 8; i++) e[i] = seen(i) ? e[i] : -INFINITY;
+        }
 #pragma unroll
-      for (int i = 0; i < 8; i++) {
-        e[i] = __builtin_amdgcn_exp2f(y[i] + base[nt]);
-        sum += e[i];
-      }
+        for (int i = 0; i < 8; i++) {
+          e[i] = __builtin_amdgcn_exp2f(e[i]);
+          sum += e[i];
+        }
+      };
+      weigh();
       // The reference moves as in attn_tile.h: where a lane's weights of a chunk have grown too large for it, or there is none.
       if (__any(sum > most[nt])) {
-        float cm = y[0];
+        float cm = -INFINITY;
 #pragma unroll
-        for (int i = 1; i < 8; i++) cm = fmaxf(cm, y[i]);
+        for (int i = 0; i < 8; i++) cm = fmaxf(cm, !edge || seen(i) ? s[nt][i / 4][i % 4] * ks[i] : -INFINITY);
         cm = max_pair(cm);
         const float old = most[nt] < 0.f ? -INFINITY : -base[nt], now = fmaxf(old, cm);
         if (now > -INFINITY) {
@@ -158,35 +175,34 @@ __device__ __forceinline__ void attn_few8(const Call& c, const AttnTile<false>& 
 #pragma unroll
           for (int dt = 0; dt < 4 * J; dt++) o[nt][dt] *= alpha;
         }
-        sum = 0.f;
-#pragma unroll
-        for (int i = 0; i < 8; i++) {
-          e[i] = __builtin_amdgcn_exp2f(y[i] + base[nt]);
-          sum += e[i];
-        }
+        weigh();
       }
       l[nt] += sum;
 #pragma unroll
-      for (int i = 0; i < 8; i++) e[i] *= w.vs[i / 4][i % 4];
+      for (int i = 0; i < 8; i++) e[i] *= wv.scale[i / 4][i % 4];
       if (edge) {  // a token that the pair does not see may have no scale
 #pragma unroll
-        for (int i = 0; i < 8; i++) e[i] = token0 + i / 4 * kBlockTokens + kg * 4 + i % 4 < limit[nt] ? e[i] : 0.f;
+        for (int i = 0; i < 8; i++) e[i] = seen(i) ? e[i] : 0.f;
       }
       uint32_t hi[4], lo[4];
 #pragma unroll
       for (int i = 0; i < 4; i++) {
+        if (!kTwo) {
+          hi[i] = pack_bf2(e[2 * i], e[2 * i + 1]);
+          continue;
+        }
         const uint32_t a = __float_as_uint(e[2 * i]), b = __float_as_uint(e[2 * i + 1]);
         hi[i] = __builtin_amdgcn_perm(b, a, 0x07060302u);  // the upper halves
         lo[i] = pack_bf2(e[2 * i] - __uint_as_float(a & 0xffff0000u), e[2 * i + 1] - __uint_as_float(b & 0xffff0000u));
       }
       p[nt][0] = as_bf16x8(u32x4_t{hi[0], hi[1], hi[2], hi[3]});
-      p[nt][1] = as_bf16x8(u32x4_t{lo[0], lo[1], lo[2], lo[3]});
+      if (kTwo) p[nt][1] = as_bf16x8(u32x4_t{lo[0], lo[1], lo[2], lo[3]});
     }
 #pragma unroll
     for (int j = 0; j < J; j++) {
 #pragma unroll
       for (int b = 0; b < kChunkBlocks; b++) {
-        u32x4_t& v = w.v[b][j];
+        u32x4_t& v = wv.code[b][j];
         // word i of lane group kg, tokens 4 i of dim tile kg, becomes tokens 4 kg of dim tile i
         u32x2_t a = __builtin_amdgcn_permlane32_swap(v[0], v[2], false, false), d = __builtin_amdgcn_permlane32_swap(v[1], v[3], false, false);
         const u32x2_t e = __builtin_amdgcn_permlane16_swap(a[0], d[0], false, false), f = __builtin_amdgcn_permlane16_swap(a[1], d[1], false, false);
@@ -200,29 +216,32 @@ __device__ __forceinline__ void attn_few8(const Call& c, const AttnTile<false>& 
       }
 #pragma unroll
       for (int i = 0; i < 4; i++) {
-        const u32x2_t lo = kv8_bf16<TYPE>(w.v[0][j][i]), hi = kv8_bf16<TYPE>(w.v[1][j][i]);
+        const u32x2_t lo = kv8_bf16<TYPE>(wv.code[0][j][i]), hi = kv8_bf16<TYPE>(wv.code[1][j][i]);
         const bf16x8_t v = as_bf16x8(u32x4_t{lo[0], lo[1], hi[0], hi[1]});
 #pragma unroll
         for (int nt = 0; nt < NT; nt++) {
           o[nt][4 * j + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[nt][0], o[nt][4 * j + i], 0, 0, 0);
-          o[nt][4 * j + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[nt][1], o[nt][4 * j + i], 0, 0, 0);
+          if (kTwo) o[nt][4 * j + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[nt][1], o[nt][4 * j + i], 0, 0, 0);
         }
         if (TYPE == kInt8) __builtin_amdgcn_sched_barrier(0);
       }
     }
+    if (n + kDepth < count) fetch_v(single, n + kDepth, wv);
   };
-  // two chunks on their way while one is worked on
-  Codes wa, wb;
-  if (count > 0) fetch(0, wa);
-  if (count > 1) fetch(1, wb);
-  for (int n = 0; n < count; n += 2) {
-    chunk(n, wa);
-    if (n + 2 < count) fetch(n + 2, wa);
-    if (n + 1 < count) {
-      chunk(n + 1, wb);
-      if (n + 3 < count) fetch(n + 3, wb);
-    }
-  }
+  auto chunks = [&](auto single) {
+#pragma unroll
+    for (int d = 0; d < kDepth; d++)
+      if (d < count) {
+        fetch_k(single, d, kw[d]);
+        fetch_v(single, d, vw[d]);
+      }
+    for (int n = 0; n < count; n += kDepth)
+#pragma unroll
+      for (int d = 0; d < kDepth; d++)
+        if (n + d < count) chunk(single, n + d, kw[d], vw[d]);
+  };
+  if (NT == 1 || x.one_tile && sides == 1) chunks(std::true_type{});
+  else chunks(std::false_type{});
   if (bad) atomicOr(c.err, SIDP_DEVERR_BLOCK);
 
   // The waves' parts, [wave][pair][dim] and their references and sums. Register r of O^T's tile dt is dim 16 dt + 4 kg + r.

@@ -100,6 +100,18 @@ __device__ __forceinline__ void load_lds16(const char* block, uint32_t offset, c
   else __builtin_amdgcn_raw_ptr_buffer_load_lds(r, to, 16, offset, 0, 0, 0);
 }
 
+// 16 bytes, or 4, a lane of a block, to registers. Buffer loads, whose address is one register a lane.
+template <int BYTES>
+__device__ __forceinline__ u32x4_t load16(const void* block, uint32_t offset, bool once) {
+  const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(block), (short)0, BYTES, 0x00020000);
+  return once ? __builtin_amdgcn_raw_buffer_load_b128(r, offset, 0, 2) : __builtin_amdgcn_raw_buffer_load_b128(r, offset, 0, 0);
+}
+template <int BYTES>
+__device__ __forceinline__ float load4(const void* block, uint32_t offset) {
+  const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(block), (short)0, BYTES, 0x00020000);
+  return __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(r, offset, 0, 0));
+}
+
 // The larger of a lane's value and its counterpart's in the other half of the wave.
 __device__ __forceinline__ float max_halves(float v) {
   const u32x2_t r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -284,9 +296,10 @@ __device__ __forceinline__ void attn_tile(const Call& c, const AttnTile<CAUSAL>&
   };
   // The 8-bit cache's scales of a chunk in LDS, [block][K, V][token]: registers 4 j .. 4 j + 3. K's are times the softmax's factor.
   float* const s_scales = (float*)(smem + 2 * kRing * kSide);
-  auto scales_of = [&](int slot, int value, int j) {
+  auto scales_at = [&](int slot, int value, int j) -> const f32x4_t& {
     return *(const f32x4_t*)(s_scales + slot * (2 * kChunk) + j / 2 * (2 * kBlockTokens) + value * kBlockTokens + half * 8 + j % 2 * 4);
   };
+  auto scales_of = [&](int slot, int value, int j) { return scales_at(slot, value, j); };
   // Where a pair's weights of a chunk have grown too large for its reference (or it has none): the reference moves to the chunk's
   // largest score, the sums with it, and the weights are made again.
   auto weigh = [&](auto parts, int slot, const f32x16_t& s, bf16x8_t (&p)[4], float sum) {
@@ -367,9 +380,17 @@ __device__ __forceinline__ void attn_tile(const Call& c, const AttnTile<CAUSAL>&
       frag[i % (kAhead + 1)] = *(const u32x4_t*)from;
     };
     float sum = 0.f, e[16];
-    f32x4_t kf[2], vf[2];  // scales, a quad of registers ahead
+    // scales, the next few registers' ahead: V's four at a time, K's too where there are registers left for it
+    constexpr int kFew = D == 64 ? 4 : 2;
+    float kf[2][kFew];
+    f32x4_t vf[2];
+    auto key_scales = [&](int i) {
+      const float* from = (const float*)&scales_at(slot, 0, i * kFew / 4) + i * kFew % 4;
+      if (kFew == 4) *(f32x4_t*)kf[i % 2] = *(const f32x4_t*)from;
+      else *(float2*)kf[i % 2] = *(const float2*)from;
+    };
     if (TYPE) {
-      kf[0] = scales_of(slot, 0, 0);
+      key_scales(0);
       vf[0] = scales_of(slot, 1, 0);
     }
 #pragma unroll
@@ -386,11 +407,9 @@ __device__ __forceinline__ void attn_tile(const Call& c, const AttnTile<CAUSAL>&
       else add(parts, f, p_last, i / 2 / DT, o[i / 2 % DT]);
 #pragma unroll
       for (int r = i * kShare; r < (i + 1) * kShare; r++) {
-        if (TYPE && r % 4 == 1 && r < 12) {  // behind the last use of the quad before
-          kf[(r / 4 + 1) % 2] = scales_of(slot, 0, r / 4 + 1);
-          vf[(r / 4 + 1) % 2] = scales_of(slot, 1, r / 4 + 1);
-        }
-        e[r] = __builtin_amdgcn_exp2f(fmaf(s[r], TYPE ? kf[r / 4 % 2][r % 4] : scale, base));
+        if (TYPE && r % kFew == 0 && r + kFew < 16) key_scales(r / kFew + 1);
+        if (TYPE && r % 4 == 1 && r < 12) vf[(r / 4 + 1) % 2] = scales_of(slot, 1, r / 4 + 1);  // behind the last use of the quad before
+        e[r] = __builtin_amdgcn_exp2f(fmaf(s[r], TYPE ? kf[r / kFew % 2][r % kFew] : scale, base));
         if (TYPE == 0) {
           if (r > 0) sum += e[r - 1];  // a step late: nothing waits for the exponential
         } else {
@@ -474,15 +493,13 @@ __device__ __forceinline__ void attn_tile(const Call& c, const AttnTile<CAUSAL>&
   if constexpr (TYPE != 0) {
     // The 8-bit cache. A thread below 2 D carries 16 bytes of a chunk's K and of its V; the last wave carries the scales.
     const int n_end = c1 - c0, code_blk = min(wave * 64 / D, kChunkBlocks - 1), code_at = t % D;
-    const bool carries = t < kChunkBlocks * D;
-    u32x4_t k_in[2], v_in[2];
-    float s_in[2];
-    int at_s = at_k;  // K is fetched two chunks before V, the scales one chunk
+    const bool carries = kChunkBlocks * D == 64 * kWaves || t < kChunkBlocks * D;
+    u32x4_t k_in[2], v_in;
+    float s_in;
     auto load_codes = [&](const uint8_t* cache, int at, int n, bool once, u32x4_t& v) {
       const int place = __builtin_amdgcn_readlane(at, n % kGroupChunks * kChunkBlocks + code_blk);
       if (!carries) return;
-      const u32x4_t* from = (const u32x4_t*)(cache + (int64_t)place * (kBlockTokens * D)) + code_at;
-      v = once ? __builtin_nontemporal_load(from) : *from;
+      v = load16<kBlockTokens * D>(cache + (int64_t)place * (kBlockTokens * D), 16 * code_at, once);
     };
     auto load_k = [&](int n, bool once, u32x4_t& v) {
       if (n > 0 && n % kGroupChunks == 0) {
@@ -491,6 +508,7 @@ __device__ __forceinline__ void attn_tile(const Call& c, const AttnTile<CAUSAL>&
       }
       load_codes(c.kv8.k, at_k, n, once, v);
     };
+    int at_s = at_k;
     auto load_v = [&](int n, bool once, u32x4_t& v) {
       if (n % kGroupChunks == 0) at_v = at_k;
       load_codes(c.kv8.v, at_v, n, once, v);
@@ -500,7 +518,8 @@ __device__ __forceinline__ void attn_tile(const Call& c, const AttnTile<CAUSAL>&
       if (wave != kWaves - 1) return;
       const int first = n % kGroupChunks * kChunkBlocks;
       const int p0 = __builtin_amdgcn_readlane(at_s, first), p1 = __builtin_amdgcn_readlane(at_s, first + 1);
-      v = c.kv8.scales[(int64_t)(half ? p1 : p0) * (2 * kBlockTokens) + col];
+      if (half) v = load4<2 * kBlockTokens * 4>(c.kv8.scales + (int64_t)p1 * (2 * kBlockTokens), 4 * col);
+      else v = load4<2 * kBlockTokens * 4>(c.kv8.scales + (int64_t)p0 * (2 * kBlockTokens), 4 * col);
     };
     auto spread = [&](u32x4_t w, char* to, int next) {  // 16 codes as bf16: eight here, eight `next` bytes on
       const u32x2_t a = kv8_bf16<TYPE>(w[0]), b = kv8_bf16<TYPE>(w[1]), d = kv8_bf16<TYPE>(w[2]), e = kv8_bf16<TYPE>(w[3]);
@@ -510,8 +529,8 @@ __device__ __forceinline__ void attn_tile(const Call& c, const AttnTile<CAUSAL>&
     auto store_k = [&](u32x4_t w, int slot) {  // a token's 16 dims
       if (carries) spread(w, smem + slot * kSide + code_blk * kBlockBytes + code_at / 16 * 512 + code_at % 16 * 16, 256);
     };
-    auto store_v = [&](u32x4_t w, int slot, int ch) {  // a dim's 16 tokens; those past kv_end become zeros (anything may stand there)
-      if ((ch + 1) * kChunk > kv_end) {
+    auto store_v = [&](auto plain, u32x4_t w, int slot, int ch) {  // a dim's 16 tokens; those past kv_end become zeros (anything may stand there)
+      if (!decltype(plain)::value && (ch + 1) * kChunk > kv_end) {
         const int left = kv_end - ch * kChunk - code_blk * kBlockTokens;
 #pragma unroll
         for (int i = 0; i < 4; i++) w[i] = left >= 4 * i + 4 ? w[i] : left <= 4 * i ? 0u : w[i] & ((1u << 8 * (left - 4 * i)) - 1u);
@@ -521,16 +540,23 @@ __device__ __forceinline__ void attn_tile(const Call& c, const AttnTile<CAUSAL>&
     // A token without a scale gets one: the rows that see it are NaN at the end.
     auto store_s = [&](float v, int slot, int ch) {
       if (wave != kWaves - 1) return;
-      const int token = ch * kChunk + half * kBlockTokens + col % kBlockTokens;
-      const bool value = col >= kBlockTokens, none = token < kv_end && v != v;
-      if (none) atomicMin(&s_odd, token);
-      if (none || token >= kv_end) v = value ? 0.f : 1.f;
+      int at = threadIdx.x;
+      asm volatile("" : "+v"(at));  // made again rather than kept, as no register is left for it
+      const int token = ch * kChunk + (at >> 5 & 1) * kBlockTokens + at % kBlockTokens;
+      const bool value = at & kBlockTokens;
+      if ((ch + 1) * kChunk > kv_end && token >= kv_end) v = 1.f;  // of a zero, or masked
+      if (__any(v != v)) {
+        if (v != v) {
+          atomicMin(&s_odd, token);
+          v = 0.f;
+        }
+      }
       // not so small that it is flushed: a masked score stays -inf
       s_scales[slot * (2 * kChunk) + lane] = value ? v : fmaxf(v * scale, 0x1p-126f);
     };
     // A turn for chunk c0 + n: K(n + 2), V(n) and the scales of n + 1 go to LDS, into the places of K(n), V(n - 2) and the scales of
-    // n - 1, and the registers that held them take K(n + 4), V(n + 2) and the scales of n + 3. odd: n's last bit. plain: every row
-    // sees the chunk whole, and there are those to fetch.
+    // n - 1, and the registers that held them take K(n + 4), V(n + 2) and the scales of n + 2, these first: they are waited for a turn
+    // before the others. odd: n's last bit. plain: every row sees the chunk whole, and there are those to fetch.
     auto turn8 = [&](auto first, auto single, auto plain, auto odd, int n, f32x16_t& s, f32x16_t& s_next, bf16x8_t (&p_last)[4],
                      bf16x8_t (&p)[4]) {
       constexpr bool kFirst = decltype(first)::value, once = decltype(single)::value, kPlain = decltype(plain)::value;
@@ -538,12 +564,12 @@ __device__ __forceinline__ void attn_tile(const Call& c, const AttnTile<CAUSAL>&
       const int ch = c0 + n;
       if (kPlain || n + 2 < n_end) store_k(k_in[kOdd], kOdd);
       __builtin_amdgcn_sched_barrier(0);
-      store_v(v_in[kOdd], kOdd, ch);
+      store_v(plain, v_in, kOdd, ch);
       __builtin_amdgcn_sched_barrier(0);
-      if (kPlain || n + 1 < n_end) store_s(s_in[1 - kOdd], 1 - kOdd, ch + 1);
+      if (kPlain || n + 1 < n_end) store_s(s_in, 1 - kOdd, ch + 1);
+      if (kPlain || n + 2 < n_end) load_s(n + 2, s_in);
+      if (kPlain || n + 1 < n_end) load_v(n + 1, once, v_in);
       if (kPlain || n + 4 < n_end) load_k(n + 4, once, k_in[kOdd]);
-      if (kPlain || n + 2 < n_end) load_v(n + 2, once, v_in[kOdd]);
-      if (kPlain || n + 3 < n_end) load_s(n + 3, s_in[1 - kOdd]);
       if (kPlain ? wave_live : ch * kChunk < wave_most) {
         if (!kPlain) mask(ch, s);
         products(first, single, kOdd, s, s_next, p_last, p);
@@ -561,17 +587,15 @@ __device__ __forceinline__ void attn_tile(const Call& c, const AttnTile<CAUSAL>&
       f32x16_t sa, sb;
       bf16x8_t pa[4], pb[4];
       if (t == 64 * (kWaves - 1)) s_odd = 0x7fffffff;  // by the wave that changes it
+      load_s(0, s_in);
       load_k(0, once, k_in[0]);
-      load_s(0, s_in[0]);
       if (1 < n_end) load_k(1, once, k_in[1]);
-      if (1 < n_end) load_s(1, s_in[1]);
-      load_v(0, once, v_in[0]);
-      if (1 < n_end) load_v(1, once, v_in[1]);
+      load_v(0, once, v_in);
       store_k(k_in[0], 0);
-      store_s(s_in[0], 0, c0);
+      store_s(s_in, 0, c0);
+      if (1 < n_end) load_s(1, s_in);
       if (1 < n_end) store_k(k_in[1], 1);
       if (2 < n_end) load_k(2, once, k_in[0]);
-      if (2 < n_end) load_s(2, s_in[0]);
       if (3 < n_end) load_k(3, once, k_in[1]);
       meet();
       if (c0 * kChunk < wave_most) {
@@ -599,8 +623,7 @@ __device__ __forceinline__ void attn_tile(const Call& c, const AttnTile<CAUSAL>&
         else add_values(single, (n_end - 1) % kRing, pb);
       }
     };
-    if (one_tile) chunks8(std::true_type{});
-    else chunks8(std::false_type{});
+    chunks8(std::false_type{});  // of several tiles: for fewer pairs there is attn_few8.h
   } else {
     if (one_tile) chunks(std::true_type{});
     else chunks(std::false_type{});

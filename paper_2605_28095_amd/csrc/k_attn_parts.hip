@@ -28,6 +28,7 @@ constexpr int kSlotsPerCu = 2;  // workgroups a CU holds
 constexpr int kMinRun = 16, kMaxRuns = 32;
 constexpr float kCutFrom = 1.75f;
 constexpr int kLeastShared = 4;  // chunks
+constexpr int kFewPairs = 64;
 
 __host__ __device__ inline int slots_of(int num_cus, int hkv) { return kSlotsPerCu * (num_cus < 1 ? 1 : num_cus) / hkv; }
 
@@ -374,7 +375,7 @@ __global__ void __launch_bounds__(256, 2) k_attn_parts(AttnPartsCall c, Layout l
       }
     };
     if (pairs <= 16) return attn_few8<D, TYPE, 1>(c, x, 1, emit);
-    if (pairs <= 64) return attn_few8<D, TYPE, 2>(c, x, pairs <= 32 ? 1 : 2, emit);
+    if (pairs <= kFewPairs) return attn_few8<D, TYPE, 2>(c, x, pairs <= 32 ? 1 : pairs <= 64 ? 2 : 4, emit);
   }
   attn_tile<D, TYPE>(c, x, [&](const AttnOut<D>& out) {
     if (rec < 0) {
