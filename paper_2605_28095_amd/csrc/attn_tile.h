@@ -100,11 +100,16 @@ __device__ __forceinline__ void load_lds16(const char* block, uint32_t offset, c
   else __builtin_amdgcn_raw_ptr_buffer_load_lds(r, to, 16, offset, 0, 0, 0);
 }
 
-// 16 bytes, or 4, a lane of a block, to registers. Buffer loads, whose address is one register a lane.
+// 16, 8 or 4 bytes a lane of a block, to registers. Buffer loads, whose address is one register a lane.
 template <int BYTES>
 __device__ __forceinline__ u32x4_t load16(const void* block, uint32_t offset, bool once) {
   const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(block), (short)0, BYTES, 0x00020000);
   return once ? __builtin_amdgcn_raw_buffer_load_b128(r, offset, 0, 2) : __builtin_amdgcn_raw_buffer_load_b128(r, offset, 0, 0);
+}
+template <int BYTES>
+__device__ __forceinline__ u32x2_t load8(const void* block, uint32_t offset, bool once) {
+  const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(block), (short)0, BYTES, 0x00020000);
+  return once ? __builtin_amdgcn_raw_buffer_load_b64(r, offset, 0, 2) : __builtin_amdgcn_raw_buffer_load_b64(r, offset, 0, 0);
 }
 template <int BYTES>
 __device__ __forceinline__ float load4(const void* block, uint32_t offset) {
@@ -623,7 +628,7 @@ __device__ __forceinline__ void attn_tile(const Call& c, const AttnTile<CAUSAL>&
         else add_values(single, (n_end - 1) % kRing, pb);
       }
     };
-    chunks8(std::false_type{});  // of several tiles: for fewer pairs there is attn_few8.h
+    chunks8(std::false_type{});  // of several tiles: for fewer pairs there is attn_few.h
   } else {
     if (one_tile) chunks(std::true_type{});
     else chunks(std::false_type{});

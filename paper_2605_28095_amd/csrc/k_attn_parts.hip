@@ -13,7 +13,7 @@
 //
 // Only whole chunks of 32 tokens are shared; the rest of the prefix is read by each
 // sequence as its own. A group shares where its tiles are at most half of its sequences'.
-#include "attn_few8.h"
+#include "attn_few.h"
 #include "attn_tile.h"
 #include "common.h"
 #include "internal.h"
@@ -25,11 +25,17 @@ namespace {
 constexpr int kSlotsPerCu = 2;  // workgroups a CU holds
 // Runs that a tile is cut into: at least this many chunks, at most this many runs, and only where the longest item is this much
 // longer than the runs would be (as in k_attn_rows.hip, which has both sides).
-constexpr int kMinRun = 16, kMaxRuns = 32;
+constexpr int kMinRun = 8, kMaxRuns = 32;
 constexpr float kCutFrom = 1.75f;
 constexpr int kLeastShared = 4;  // chunks
+// Over codes, tiles of up to this many pairs go by attn_few.h, whose waves spread out what they need by themselves (16 sequences of
+// e4m3 over 4000, 5 rows 56 us, 62 by attn_tile.h, 8 rows 61 and 63; 16 rows 96 and 81). Over bf16, 64 pairs over 2048 shared tokens
+// 29 us by it, 26 by attn_tile.h: only 16 pairs go by it.
 constexpr int kFewPairs = 64;
+// Wave items: of at most kWaveShare / 4 of the chunks that a wave has on average, or kWaveLeast.
+constexpr int kWaveShare = 5, kWaveLeast = 4;
 
+__host__ __device__ inline int half_places(int num_cus) { return kSlotsPerCu * (num_cus < 1 ? 1 : num_cus) / 2; }
 __host__ __device__ inline int slots_of(int num_cus, int hkv) { return kSlotsPerCu * (num_cus < 1 ? 1 : num_cus) / hkv; }
 
 enum { kOwnKeys = 1, kOneTile = 2 };  // flags: a row sees the keys up to its own; nobody else reads these keys
@@ -83,14 +89,16 @@ Layout layout_of(int batch, int max_rows, int hq, int hkv, int d, int num_cus, b
 // every tile is cut into even runs of at most `run` chunks, the shortest of kTries
 // lengths between an even share of all chunks and one that cannot give more runs than
 // fit. Otherwise sequences' tiles stay whole, groups' are cut into runs of half an even
-// share, and the longest items come first, so that the launch ends evenly.
+// share, and the longest items come first, so that the launch ends evenly. Tiles of few
+// pairs that are short beside a wave's even share are items of a wave each: they are
+// listed apart, behind the others.
 constexpr int kTries = 8;
 constexpr int kPlanWaves = 16;
 __global__ void __launch_bounds__(64 * kPlanWaves) k_attn_parts_plan(AttnPartsCall c, Layout lay) {
   extern __shared__ int32_t s_lds[];
   __shared__ int s_scan[4][kPlanWaves], s_longest[kPlanWaves];
   __shared__ uint32_t s_total[kPlanWaves];
-  __shared__ int s_hist[256];
+  __shared__ int s_hist[256], s_waves[256], s_listed[2];
   __shared__ int s_items[kTries];
   __shared__ int s_cuts, s_bad;
   const int t = threadIdx.x, wave = t >> 6, lane = t & 63, threads = blockDim.x, waves = threads / 64;
@@ -111,7 +119,7 @@ __global__ void __launch_bounds__(64 * kPlanWaves) k_attn_parts_plan(AttnPartsCa
   Cut* cuts = (Cut*)(ws + lay.cuts);
   if (t < kTries) s_items[t] = 0;
   if (t == 0) s_cuts = s_bad = 0;
-  for (int i = t; i < 256; i += threads) s_hist[i] = 0;
+  for (int i = t; i < 256; i += threads) s_hist[i] = s_waves[i] = 0;
   __syncthreads();
   // a sequence whose starts or lengths the call does not cover has no rows
   bool bad = false;
@@ -225,15 +233,19 @@ __global__ void __launch_bounds__(64 * kPlanWaves) k_attn_parts_plan(AttnPartsCa
     const int b = i - G, end = min(s_rows[b], (place + 1) * tm), from = s_group[b] >= 0 ? s_chunks[s_group[b]] : 0;
     return Tile{i, place, end - place * tm, from, (s_ctx[b] + end + kChunk - 1) / kChunk - from, s_group[b] >= 0};
   };
-  // the tiles of this thread, in order
+  // the tiles of this thread, in order; one, as a rule, which is looked up once
   const int per = (tiles + threads - 1) / threads, n0 = min(t * per, tiles), n1 = min(n0 + per, tiles);
+  Tile only = {};
+  if (per == 1 && n0 < n1) only = tile_of(n0);
+  auto each_tile = [&](auto f) {
+    for (int n = n0; n < n1; n++) f(per == 1 ? only : tile_of(n));
+  };
   uint32_t total = 0;
   int longest = 1;
-  for (int n = n0; n < n1; n++) {
-    const int chunks = tile_of(n).chunks;
-    total += chunks;
-    longest = max(longest, chunks);
-  }
+  each_tile([&](const Tile& x) {
+    total += x.chunks;
+    longest = max(longest, x.chunks);
+  });
   const uint32_t own_chunks = total;
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) {
@@ -278,30 +290,34 @@ __global__ void __launch_bounds__(64 * kPlanWaves) k_attn_parts_plan(AttnPartsCa
   auto parts_of = [&](const Tile& x) { return few || x.i < G ? (x.chunks + run - 1) / run : 1; };
   // places of entries (in order, or by length) and of records
   auto bucket = [&](const Tile& x, int parts) { return 255 - x.chunks / parts * 255 / longest; };
+  const int wave_most = max((int)(total / (kWaves * max(slots, 1))) * kWaveShare / 4, kWaveLeast);
+  auto by_wave = [&](const Tile& x) {
+    return !few && x.i >= G && x.rows * group <= 16 && (c.kv8.type != 0 || x.rows == 1) && x.chunks <= wave_most;
+  };
   int entries_mine = 0, recs_mine = 0, all, recs;
-  for (int n = n0; n < n1; n++) {
-    const Tile x = tile_of(n);
+  each_tile([&](const Tile& x) {
     const int parts = parts_of(x);
     entries_mine += parts;
     if (parts > 1 || x.rec) recs_mine += parts * x.rows;
-    if (!few) atomicAdd(&s_hist[bucket(x, parts)], parts);
-  }
+    if (!few) atomicAdd(by_wave(x) ? &s_waves[bucket(x, 1)] : &s_hist[bucket(x, parts)], parts);
+  });
   int at = scan(entries_mine, 2, all), rec_at = scan(recs_mine, 3, recs);
   {  // a group's first record
     int r = rec_at;
-    for (int n = n0; n < n1; n++) {
-      const Tile x = tile_of(n);
+    each_tile([&](const Tile& x) {
       if (x.i < G && x.place == 0) s_own[x.i] = r;
-      if (parts_of(x) > 1 || x.rec) r += parts_of(x) * x.rows;
-    }
+      const int parts = parts_of(x);
+      if (parts > 1 || x.rec) r += parts * x.rows;
+    });
   }
   __syncthreads();
-  if (!few && t < 64) {
+  if (!few && t < 128) {  // a wave each
+    int* hist = t < 64 ? s_hist : s_waves;
     int h[4], sum = 0;
 #pragma unroll
     for (int j = 0; j < 4; j++) {
       h[j] = sum;
-      sum += s_hist[4 * t + j];
+      sum += hist[4 * lane + j];
     }
     int inc = sum;
 #pragma unroll
@@ -310,11 +326,12 @@ __global__ void __launch_bounds__(64 * kPlanWaves) k_attn_parts_plan(AttnPartsCa
       if (lane >= o) inc += v;
     }
 #pragma unroll
-    for (int j = 0; j < 4; j++) s_hist[4 * t + j] = inc - sum + h[j];
+    for (int j = 0; j < 4; j++) hist[4 * lane + j] = inc - sum + h[j];
+    if (lane == 63) s_listed[t >> 6] = inc;
   }
   __syncthreads();
-  for (int n = n0; n < n1; n++) {
-    const Tile x = tile_of(n);
+  const int by_group = few ? all : s_listed[0];  // items of a workgroup
+  each_tile([&](const Tile& x) {
     const int parts = parts_of(x);
     const bool shared = x.i < G, rec = parts > 1 || x.rec;
     const int b = shared ? s_seq[x.i] : x.i - G;
@@ -322,7 +339,7 @@ __global__ void __launch_bounds__(64 * kPlanWaves) k_attn_parts_plan(AttnPartsCa
     const int end = shared ? x.chunks * kChunk : s_ctx[b] + x.place * tm + x.rows;
     const bool alone = (shared ? s_grows[x.i] : s_rows[b]) <= tm;
     // Within a step of length the order is whatever the atomics give; items write places of their own, so results do not depend on it.
-    const int e0 = few ? at : atomicAdd(&s_hist[bucket(x, parts)], parts);
+    const int e0 = few ? at : by_wave(x) ? by_group + atomicAdd(&s_waves[bucket(x, 1)], 1) : atomicAdd(&s_hist[bucket(x, parts)], parts);
     for (int p = 0; p < parts; p++) {
       const int lo = x.from + x.chunks * p / parts, hi = x.from + x.chunks * (p + 1) / parts;
       entries[e0 + p] = Entry{b, row0, x.rows, shared ? end - 1 : end - x.rows, end, (uint32_t)lo | (uint32_t)(hi - lo) << 16,
@@ -341,48 +358,63 @@ __global__ void __launch_bounds__(64 * kPlanWaves) k_attn_parts_plan(AttnPartsCa
     }
     at += parts;
     if (rec) rec_at += parts * x.rows;
-  }
+  });
   __syncthreads();
   if (t == 0) {
-    counts[0] = all;
+    counts[0] = by_group;
     counts[1] = s_cuts;
+    counts[2] = all - by_group;
   }
 }
 
+// Workgroups, in the order in which they start: half the chip's places of workgroups' items, then as many of wave items as go beside
+// them, and again; the former are products most of all, the latter bytes.
 template <int D, int TYPE>
 __global__ void __launch_bounds__(256, 2) k_attn_parts(AttnPartsCall c, Layout lay) {
   const char* ws = (const char*)c.ws;
-  const int hkv = c.kv.hkv, item = blockIdx.x;
-  if (item >= ((cint32_t*)ws)[0] * hkv) return;
-  cint32_t* ep = (cint32_t*)(ws + lay.entries) + (item / hkv) * 8;
-  const int c0 = ep[5] & 0xffff, rec = ep[6], flags = ep[7];
-  const AttnTile<false> x = {ep[0], ep[1], ep[2], ep[3], ep[4], c0, c0 + (int)((uint32_t)ep[5] >> 16), item % hkv,
+  const int hkv = c.kv.hkv, group = c.hq / hkv;
+  const int items = ((cint32_t*)ws)[0] * hkv, wave_items = ((cint32_t*)ws)[2] * hkv, wave_groups = (wave_items + kWaves - 1) / kWaves;
+  int item = blockIdx.x, wave_group = -1;
+  if (wave_groups > 0) {
+    const int half = half_places(c.num_cus), rounds = items / half;
+    const int beside = items == 0 ? 0 : (int)(((int64_t)wave_groups * half + items - 1) / items);
+    const int round = min(item / (half + beside), rounds), in_round = item - round * (half + beside);
+    const int here = round < rounds ? half : items - rounds * half;  // the last round takes what is left of both
+    if (in_round < here) item = round * half + in_round;
+    else wave_group = round * beside + in_round - here;
+  }
+  if (wave_group < 0 ? item >= items : wave_group >= wave_groups) return;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int at = wave_group < 0 ? item : items + wave_group * kWaves + wave;  // among all items, entry by entry
+  if (at >= items + wave_items) return;
+  cint32_t* ep = (cint32_t*)(ws + lay.entries) + (at / hkv) * 8;
+  const int c0 = ep[5] & 0xffff, rec = ep[6], flags = ep[7], g = at % hkv;
+  const AttnTile<false> x = {ep[0], ep[1], ep[2], ep[3], ep[4], c0, c0 + (int)((uint32_t)ep[5] >> 16), g,
                              (flags & kOneTile) != 0, flags & kOwnKeys};
   float* const recs = (float*)((char*)c.ws + lay.recs);
   float* const sums = (float*)((char*)c.ws + lay.sums);
+  const int pairs = x.tokens * group;
+  auto emit = [&](int tok, int head, int dim, f32x4_t o, float sum, float ref) {
+    if (rec < 0) {
+      const float inv = 1.f / sum;
+      *(u32x2_t*)(c.out + ((int64_t)(x.row0 + tok) * c.hq + g * group + head) * D + dim) =
+          u32x2_t{pack_bf2(o[0] * inv, o[1] * inv), pack_bf2(o[2] * inv, o[3] * inv)};
+    } else {
+      const int64_t to = (int64_t)(rec + tok) * c.hq + g * group + head;
+      *(f32x4_t*)(recs + to * D + dim) = o;
+      if (dim == 0) *(float2*)(sums + to * 2) = make_float2(ref, sum);
+    }
+  };
+  if (pairs <= 16 && (TYPE != 0 || x.tokens == 1 || x.step == 0)) return attn_few<D, TYPE, 1>(c, x, wave_group < 0 ? 1 : 0, emit);
   if constexpr (TYPE != 0) {
-    const int group = c.hq / hkv, pairs = x.tokens * group;
-    auto emit = [&](int tok, int head, int dim, f32x4_t o, float sum, float ref) {
-      const int at = item % hkv * group + head;
-      if (rec < 0) {
-        const float inv = 1.f / sum;
-        *(u32x2_t*)(c.out + ((int64_t)(x.row0 + tok) * c.hq + at) * D + dim) =
-            u32x2_t{pack_bf2(o[0] * inv, o[1] * inv), pack_bf2(o[2] * inv, o[3] * inv)};
-      } else {
-        const int64_t to = (int64_t)(rec + tok) * c.hq + at;
-        *(f32x4_t*)(recs + to * D + dim) = o;
-        if (dim == 0) *(float2*)(sums + to * 2) = make_float2(ref, sum);
-      }
-    };
-    if (pairs <= 16) return attn_few8<D, TYPE, 1>(c, x, 1, emit);
-    if (pairs <= kFewPairs) return attn_few8<D, TYPE, 2>(c, x, pairs <= 32 ? 1 : pairs <= 64 ? 2 : 4, emit);
+    if (pairs <= kFewPairs) return attn_few<D, TYPE, 2>(c, x, pairs <= 32 ? 1 : 2, emit);
   }
   attn_tile<D, TYPE>(c, x, [&](const AttnOut<D>& out) {
     if (rec < 0) {
       out.rows(c.out);
     } else {
-      const int64_t at = out.row + (int64_t)(rec - x.row0) * c.hq;  // the same head of the record
-      out.record(recs + at * D, sums + at * 2);
+      const int64_t to = out.row + (int64_t)(rec - x.row0) * c.hq;  // the same head of the record
+      out.record(recs + to * D, sums + to * 2);
     }
   });
 }
@@ -440,6 +472,12 @@ __global__ void __launch_bounds__(256) k_attn_parts_join(AttnPartsCall c, Layout
   }
 }
 
+// Workgroups: as many as there can be items, and one for each round of them, whose wave items are rounded up.
+int64_t grid_of(const Layout& l, int hkv, int num_cus) {
+  const int64_t items = (int64_t)l.entries_cap * hkv;
+  return items + items / half_places(num_cus) + 2;
+}
+
 hipError_t allow_lds(const void* kernel, size_t lds) {
   return lds > 32 * 1024 ? hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) : hipSuccess;
 }
@@ -447,14 +485,14 @@ hipError_t allow_lds(const void* kernel, size_t lds) {
 template <int D, int TYPE>
 hipError_t launch_type(const AttnPartsCall& c, hipStream_t s) {
   const Layout lay = layout_of(c.batch, c.max_rows, c.hq, c.kv.hkv, D, c.num_cus, c.groups > 0);
-  const int waves = std::min(kPlanWaves, (std::max(c.batch, lay.tiles_cap + (c.groups > 0 ? lay.tiles_cap / 2 : 0)) + 63) / 64);
+  const int waves = std::max(2, std::min(kPlanWaves, (std::max(c.batch, lay.tiles_cap + (c.groups > 0 ? lay.tiles_cap / 2 : 0)) + 63) / 64));
   const size_t plan_lds = (4 * (size_t)c.batch + 5 * (size_t)c.groups + 1) * sizeof(int32_t);
   hipError_t e = allow_lds((const void*)k_attn_parts_plan, plan_lds);
-  constexpr int lds = TYPE ? std::max(tile_lds<D, TYPE>(), few_lds<D, 2>()) : tile_lds<D, TYPE>();
+  constexpr int lds = std::max(tile_lds<D, TYPE>(), few_lds<D, TYPE ? 2 : 1>());
   if (e == hipSuccess) e = allow_lds((const void*)k_attn_parts<D, TYPE>, lds);
   if (e != hipSuccess) return e;
   k_attn_parts_plan<<<1, 64 * waves, plan_lds, s>>>(c, lay);
-  k_attn_parts<D, TYPE><<<(unsigned)((int64_t)lay.entries_cap * c.kv.hkv), 256, lds, s>>>(c, lay);
+  k_attn_parts<D, TYPE><<<(unsigned)grid_of(lay, c.kv.hkv, c.num_cus), 256, lds, s>>>(c, lay);
   // workgroups a cut and KV head: as many as its rows need, or as fill the chip
   const int most = (std::min(tile_tokens(c.hq / c.kv.hkv), c.max_rows) * (c.hq / c.kv.hkv) + 1024 / D - 1) / (1024 / D);
   const int z = std::max<int64_t>(1, std::min<int64_t>(most, 4 * (int64_t)c.num_cus / std::max<int64_t>(1, (int64_t)lay.cuts_cap * c.kv.hkv)));
@@ -471,7 +509,7 @@ hipError_t launch_d(const AttnPartsCall& c, hipStream_t s) {
 // 0 for more items than one launch covers: HIP's have fewer than 2^32 threads.
 size_t attn_parts_ws_bytes(int batch, int max_rows, int hq, int hkv, int d, int num_cus, bool groups) {
   const Layout l = layout_of(batch, max_rows, hq, hkv, d, num_cus, groups);
-  return (int64_t)l.entries_cap * hkv * 256 < (int64_t)1 << 32 ? l.bytes : 0;
+  return grid_of(l, hkv, num_cus) * 256 < (int64_t)1 << 32 ? l.bytes : 0;
 }
 
 hipError_t launch_attention_parts(const AttnPartsCall& c, hipStream_t s) {
