@@ -63,12 +63,12 @@ Layout layout_of(int batch, int max_rows, int hq, int hkv, int d, int num_cus, b
   Layout l;
   l.tiles_cap = (int)std::min<int64_t>(max_rows, (int64_t)max_rows / tm + std::min(batch, max_rows));
   // A group's tiles are at most half of its sequences'. With fewer tiles than slots runs are chosen so that they fit the slots;
-  // with more only shared tiles are cut, into runs of at least half an even share of all chunks.
-  l.entries_cap = std::max(l.tiles_cap, slots) + (groups ? l.tiles_cap / 2 + 2 * slots : 0);
+  // with more only shared tiles are cut, into runs of an even share of all chunks or more.
+  l.entries_cap = std::max(l.tiles_cap, slots) + (groups ? l.tiles_cap / 2 + slots : 0);
   l.cuts_cap = groups ? l.tiles_cap : std::min(l.tiles_cap, std::max(slots, 0));
   // 2 ceil(R / tm) <= sum ceil(rows / tm) <= R / tm + sequences: R of the groups that share is at most tm a sequence
   const int64_t shared = groups ? 2 * std::min<int64_t>(max_rows, (int64_t)batch * tm) : 0;
-  l.recs_cap = (int)(shared + (int64_t)(groups ? 2 : 1) * slots * std::min(tm, max_rows));
+  l.recs_cap = (int)(shared + (int64_t)slots * std::min(tm, max_rows));
   size_t o = 64;
   auto place = [&](size_t n) {
     const size_t at = o;
@@ -88,8 +88,9 @@ Layout layout_of(int batch, int max_rows, int hq, int hkv, int d, int num_cus, b
 // Tiles are numbered groups first, then sequences. Fewer than the chip holds at once:
 // every tile is cut into even runs of at most `run` chunks, the shortest of kTries
 // lengths between an even share of all chunks and one that cannot give more runs than
-// fit. Otherwise sequences' tiles stay whole, groups' are cut into runs of half an even
-// share, and the longest items come first, so that the launch ends evenly. Tiles of few
+// fit. Otherwise sequences' tiles stay whole, groups' are cut into runs of an even share
+// (256 sequences under 8192 tokens 142 us, 150 with half of one, whose records are twice
+// as many; 72 under 6 prefixes 51 and 57), and the longest items come first, so that the launch ends evenly. Tiles of few
 // pairs that are short beside a wave's even share are items of a wave each: they are
 // listed apart, behind the others.
 constexpr int kTries = 8;
@@ -285,7 +286,7 @@ __global__ void __launch_bounds__(64 * kPlanWaves) k_attn_parts_plan(AttnPartsCa
       run = min(run, try_of(j));
     }
   } else if (gtiles > 0 && slots > 0) {
-    run = min(longest, max((int)(total / (2 * slots)) + 1, kMinRun));
+    run = min(longest, max((int)(total / slots) + 1, kMinRun));
   }
   auto parts_of = [&](const Tile& x) { return few || x.i < G ? (x.chunks + run - 1) / run : 1; };
   // places of entries (in order, or by length) and of records
