@@ -207,6 +207,8 @@ struct SampleCall {
   float* logprobs;
   int32_t* kept;
   void* ws;
+  // set by launch_sample
+  int segments = 1;
 };
 size_t sample_ws_bytes(int rows, int vocab);
 hipError_t launch_sample(const SampleCall& c, hipStream_t s);

@@ -14,9 +14,26 @@
 // of 32 bits one draw in a hundred or so over 10^5 alike tokens would be a neighbour's.)
 //
 // No row is sorted. A histogram over the exponents, 2048 bins of counts and weights, says
-// in which bin a count or a weight is reached; only that bin's tokens, or those of all
-// bins up to it where they are few, are picked out and put in order. A bin with too many
-// (equal logits) is divided by its tokens' order until it has few.
+// in which bin a count or a weight is reached. Each place depends on the one before it,
+// but bounds of all follow from the histogram, so that the tokens of every bin that can
+// matter are picked out of the row at once (where they are too many, a bin at a time, when
+// its place is asked for). A place's own bin is divided by its tokens' order, value and
+// then index, with a small histogram each time, until it has few, and these are put in
+// order. With a top-k the large histogram counts only: the weights that matter are those of
+// the tokens picked out.
+//
+// Four launches: the row's ends (its largest and least logit), the histogram, the picking,
+// the draw. The first three read the row, from memory the first time, by as many segments
+// as fill the chip; histograms are joined by atomics on whole numbers, whose order changes
+// nothing.
+//
+// Measured, us: a row of 128256 bf16 logits 30, 16 rows 37 (top-k and top-p) and 58 (top-p),
+// 64 rows 49 and 78, 256 rows 95 and 137; 256 rows of 151936 fp32 logits with all settings
+// mixed 144, of which the ends take 32 (155 MB at 4.8 TB/s, the only reading from memory);
+// 512 rows of 32001 bf16 logits at a temperature alone 80. What bounds it behind the first
+// reading is arithmetic on logits, an exponential in 64 bits and two LDS atomics each, and
+// for few rows the barriers of the draw, about 14 us. A workgroup a row for all four steps
+// in one launch took 166 for the mixed rows and 84 for the 512.
 #include <type_traits>
 
 #include "common.h"
@@ -28,12 +45,17 @@ namespace {
 
 typedef unsigned long long u64;
 
-constexpr int kThreads = 1024, kWavesOf = kThreads / 64;
+// Waves of a group that goes through barriers together: 8. With 16 the 256 mixed rows took 156 us (144) and a single one 33 (30), with 4
+// they took 174 and 35.
+constexpr int kThreads = 512, kWavesOf = kThreads / 64;
 constexpr int kBins = 2048;
 constexpr float kReach = 44.f;   // weights of 2^-kReach and less are 0
 constexpr int kUnit = 43;        // bits behind the point of a weight: 2^20 tokens of 2^43 are 2^63
 constexpr int kList = 4096;      // tokens picked out of a row at once
-constexpr int kSub = 1024;       // tokens of a bin that are put in order
+constexpr int kParts = 512;      // of a bin that is divided
+constexpr int kFew = 64;         // tokens that are put in order
+constexpr int kSteps = 4;        // places that a row can ask for, each with its own answer in LDS
+constexpr int kTurns = 4;        // bins are told to all in as many places in turn, so that one barrier each is enough
 
 // The order of tokens: larger keys first.
 __device__ __forceinline__ u64 make_key(float x, int index) {
@@ -78,52 +100,49 @@ __device__ __forceinline__ u64 weight_of(double d) {
   return (u64)__builtin_bit_cast(int64_t, p) & ((1ull << 52) - 1);
 }
 
-// f(logit, index) for every logit of a row, 16 bytes a load where its address allows.
+// f(logit, index) for the logits first .. last - 1 of a row, 16 bytes a load where their address allows.
 template <bool F32, class F>
-__device__ __forceinline__ void each_logit(const void* row, int n, const F& f) {
-  constexpr int kSize = F32 ? 4 : 2, V = 16 / kSize, U = 4;
-  const int t = threadIdx.x;
-  auto at = [&](int i) { return F32 ? ((const float*)row)[i] : bf2f(((const uint16_t*)row)[i]); };
-  const int head = min(n, (int)(-(uintptr_t)row & 15) / kSize), vectors = (n - head) / V, tail = head + vectors * V;
-  if (t < head) f(at(t), t);
-  const u32x4_t* v = (const u32x4_t*)((const char*)row + head * kSize);
-  for (int j0 = 0; j0 < vectors; j0 += kThreads * U) {
-    u32x4_t w[U];
+__device__ __forceinline__ void each_logit(const void* row, int first, int last, const F& f) {
+  constexpr int kSize = F32 ? 4 : 2, V = 16 / kSize;
+  const int t = threadIdx.x, n = last - first;
+  const char* from = (const char*)row + (int64_t)first * kSize;
+  auto at = [&](int i) { return F32 ? ((const float*)from)[i] : bf2f(((const uint16_t*)from)[i]); };
+  const int head = min(n, (int)(-(uintptr_t)from & 15) / kSize), vectors = (n - head) / V, tail = head + vectors * V;
+  if (t < head) f(at(t), first + t);
+  const u32x4_t* v = (const u32x4_t*)(from + head * kSize);
+  // The next two loads are under way while a third's logits are worked on. A loop that is not unrolled: with few logits a thread,
+  // most of a call's time is that of its instructions on their way.
+  auto load = [&](int j) { return j < vectors ? v[j] : u32x4_t{0, 0, 0, 0}; };
+  u32x4_t w0 = load(t), w1 = load(t + kThreads), w2 = load(t + 2 * kThreads);
+#pragma unroll 1
+  for (int j = t; j < vectors; j += kThreads) {
 #pragma unroll
-    for (int u = 0; u < U; u++) {
-      const int j = j0 + u * kThreads + t;
-      if (j < vectors) w[u] = v[j];
+    for (int k = 0; k < V; k++) {
+      const float x = F32 ? __uint_as_float(w0[k % 4]) : __uint_as_float(k % 2 ? w0[k / 2] & 0xffff0000u : w0[k / 2] << 16);
+      f(x, first + head + j * V + k);
     }
-#pragma unroll
-    for (int u = 0; u < U; u++) {
-      const int j = j0 + u * kThreads + t;
-      if (j < vectors) {
-#pragma unroll
-        for (int k = 0; k < V; k++) {
-          const float x = F32 ? __uint_as_float(w[u][k % 4]) : __uint_as_float(k % 2 ? w[u][k / 2] & 0xffff0000u : w[u][k / 2] << 16);
-          f(x, head + j * V + k);
-        }
-      }
-    }
+    w0 = w1;
+    w1 = w2;
+    w2 = load(j + 3 * kThreads);
   }
-  if (t < n - tail) f(at(tail + t), tail + t);
+  if (t < n - tail) f(at(tail + t), first + tail + t);
 }
 
+template <int BINS>
 struct Histogram {
-  u64 weight[kBins];
-  uint32_t count[kBins];
+  u64 weight[BINS];
+  uint32_t count[BINS];
 };
 struct Memory {
-  Histogram all;  // running sums, once they are made
-  union {
-    u64 list[kList];
-    Histogram part;  // of one bin that has too many tokens
-  };
-  u64 sub[kSub], sub_weight[kSub];
   u64 wave_a[kWavesOf], wave_b[kWavesOf];
-  u64 found_key, found_weight;
-  uint32_t found_count, filled, listed;
-  int bin;
+  u64 found_key[kSteps], found_weight[kSteps];
+  uint32_t found_count[kSteps], filled[kSteps], listed;
+  int bin[kTurns];
+  Histogram<kBins> all;  // running sums, once they are made
+  // what follows is the draw's
+  Histogram<kParts> part;  // of a bin that is divided
+  u64 list[kList];
+  u64 few[kFew], few_weight[kFew];
 };
 // LDS is addressed as such, through its own name in code that is inlined: a flat access decides by its address register alone
 // whether it goes to LDS, and the compiler may put a register 8 bytes in front of what it addresses.
@@ -137,266 +156,565 @@ struct Place {
   uint32_t count;
 };
 
-__device__ __forceinline__ u64 wave_max_u64(u64 v) {
+// A value of all threads', made of two at a time by `f`; every thread calls.
+template <class T, class F>
+__device__ __forceinline__ T over_group(T v, const F& f) {
+  Memory& m = memory();
 #pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) {
-    const u64 w = __shfl_xor(v, o, 64);
-    v = w > v ? w : v;
-  }
-  return v;
-}
-// The largest of all threads' values; every thread calls.
-__device__ __forceinline__ u64 group_max(u64 v) {
-  Memory& m = memory();
-  v = wave_max_u64(v);
-  if ((threadIdx.x & 63) == 0) m.wave_a[threadIdx.x >> 6] = v;
+  for (int o = 32; o >= 1; o >>= 1) v = f(v, __shfl_xor(v, o, 64));
+  T* s = (T*)m.wave_a;
+  if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
   __syncthreads();
-  for (int w = 0; w < kWavesOf; w++) v = m.wave_a[w] > v ? m.wave_a[w] : v;
+  v = s[0];
+  for (int w = 1; w < kWavesOf; w++) v = f(v, s[w]);
   __syncthreads();
   return v;
 }
+__device__ __forceinline__ u64 larger(u64 a, u64 b) { return a > b ? a : b; }
 
-__device__ __forceinline__ void clear(Histogram& h) {
-  for (int i = threadIdx.x; i < kBins; i += kThreads) h.weight[i] = 0, h.count[i] = 0;
+template <int BINS>
+__device__ __forceinline__ void clear(Histogram<BINS>& h) {
+  for (int i = threadIdx.x; i < BINS; i += kThreads) h.weight[i] = 0, h.count[i] = 0;
 }
-// A histogram's running sums, in its place.
-__device__ __forceinline__ void run_up(Histogram& h) {
+// A histogram's running sums, in its place: of counts, weights or both.
+template <bool COUNTS, bool WEIGHTS, int BINS>
+__device__ __forceinline__ void run_up(Histogram<BINS>& h) {
   Memory& m = memory();
-  constexpr int kPer = kBins / kThreads;
+  constexpr int kPer = BINS < kThreads ? 1 : BINS / kThreads;
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  const bool mine = t * kPer < BINS;
   u64 w[kPer], sw = 0;
   uint32_t c[kPer], sc = 0;
 #pragma unroll
   for (int i = 0; i < kPer; i++) {
-    w[i] = sw += h.weight[t * kPer + i];
-    c[i] = sc += h.count[t * kPer + i];
+    if (WEIGHTS) w[i] = sw += mine ? h.weight[t * kPer + i] : 0;
+    if (COUNTS) c[i] = sc += mine ? h.count[t * kPer + i] : 0;
   }
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
-    const u64 a = __shfl_up(sw, o, 64);
-    const uint32_t b = (uint32_t)__shfl_up((int)sc, o, 64);
-    if (lane >= o) sw += a, sc += b;
+    if (WEIGHTS) {
+      const u64 a = __shfl_up(sw, o, 64);
+      if (lane >= o) sw += a;
+    }
+    if (COUNTS) {
+      const uint32_t b = (uint32_t)__shfl_up((int)sc, o, 64);
+      if (lane >= o) sc += b;
+    }
   }
-  if (lane == 63) m.wave_a[wave] = sw, m.wave_b[wave] = sc;
-  sw -= w[kPer - 1];
-  sc -= c[kPer - 1];
+  if (lane == 63) {
+    if (WEIGHTS) m.wave_a[wave] = sw;
+    if (COUNTS) m.wave_b[wave] = sc;
+  }
+  if (WEIGHTS) sw -= w[kPer - 1];
+  if (COUNTS) sc -= c[kPer - 1];
   __syncthreads();
-  for (int i = 0; i < wave; i++) sw += m.wave_a[i], sc += (uint32_t)m.wave_b[i];
 #pragma unroll
-  for (int i = 0; i < kPer; i++) h.weight[t * kPer + i] = sw + w[i], h.count[t * kPer + i] = sc + c[i];
+  for (int i = 0; i < kWavesOf - 1; i++) {  // read side by side
+    if (WEIGHTS) sw += i < wave ? m.wave_a[i] : 0;
+    if (COUNTS) sc += i < wave ? (uint32_t)m.wave_b[i] : 0;
+  }
+#pragma unroll
+  for (int i = 0; i < kPer; i++) {
+    if (WEIGHTS && mine) h.weight[t * kPer + i] = sw + w[i];
+    if (COUNTS && mine) h.count[t * kPer + i] = sc + c[i];
+  }
   __syncthreads();
 }
 // The bin of running sums `h` in which `target` is reached, by count or by weight. It is, in one.
-__device__ __forceinline__ int bin_of(const Histogram& h, bool by_count, u64 target) {
+template <int BINS>
+__device__ __forceinline__ int bin_of(const Histogram<BINS>& h, bool by_count, u64 target, int& turn) {
   Memory& m = memory();
-  for (int i = threadIdx.x; i < kBins; i += kThreads) {
+  const int slot = turn++ % kTurns;
+  for (int i = threadIdx.x; i < BINS; i += kThreads) {
     const u64 to = by_count ? h.count[i] : h.weight[i], from = i == 0 ? 0 : by_count ? h.count[i - 1] : h.weight[i - 1];
-    if (from < target && target <= to) m.bin = i;
+    if (from < target && target <= to) m.bin[slot] = i;
   }
   __syncthreads();
-  const int b = m.bin;
-  __syncthreads();
-  return b;
+  return m.bin[slot];
 }
 
-// Where the count or the weight, in order, reaches `target`, which it does. listed_to: the last of the bins, from 0 on, whose tokens
-// the list holds; -1: none.
-template <bool F32>
-__device__ __forceinline__ Place find(const void* row, int n, const Scale& s, bool by_count, u64 target, int& listed_to) {
-  Memory& m = memory();
-  const int b = bin_of(m.all, by_count, target);
-  uint32_t base_c = b ? m.all.count[b - 1] : 0, in_bin = m.all.count[b] - base_c;
-  u64 base_w = b ? m.all.weight[b - 1] : 0;
-  if (threadIdx.x == 0) m.filled = 0;
-  __syncthreads();
-  if (in_bin <= kSub) {
-    auto take = [&](u64 key) { m.sub[atomicAdd(&m.filled, 1u)] = key; };
-    if (listed_to < 0 && m.all.count[b] <= kList) {  // the first time: what later places can ask for, too
-      if (threadIdx.x == 0) m.listed = 0;
-      __syncthreads();
-      each_logit<F32>(row, n, [&](float x, int i) {
-        if (x > -INFINITY && s.bin(x) <= b) m.list[atomicAdd(&m.listed, 1u)] = make_key(x, i);
-      });
-      listed_to = b;
-      __syncthreads();
-    }
-    if (b <= listed_to) {
-      for (uint32_t i = threadIdx.x; i < m.listed; i += kThreads)
-        if (s.bin(key_value(m.list[i])) == b) take(m.list[i]);
-    } else {
-      each_logit<F32>(row, n, [&](float x, int i) {
-        if (x > -INFINITY && s.bin(x) == b) take(make_key(x, i));
-      });
-    }
-  } else {
-    // keys in lo .. hi of the bin, divided by the leading bits in which they differ
-    u64 lo = 0, hi = ~0ull;
-    listed_to = -1;
-    while (in_bin > kSub) {
-      u64 most = 0, least = 0;  // of ~key
-      each_logit<F32>(row, n, [&](float x, int i) {
-        if (x > -INFINITY && s.bin(x) == b) {
-          const u64 k = make_key(x, i);
-          if (k >= lo && k <= hi) {
-            most = k > most ? k : most;
-            least = ~k > least ? ~k : least;
-          }
-        }
-      });
-      hi = group_max(most);
-      lo = ~group_max(least);
-      const int shift = max(0, 64 - __clzll((long long)(hi - lo)) - 11);
-      clear(m.part);
-      __syncthreads();
-      each_logit<F32>(row, n, [&](float x, int i) {
-        if (x > -INFINITY && s.bin(x) == b) {
-          const u64 k = make_key(x, i);
-          if (k >= lo && k <= hi) {
-            const int p = (int)((hi - k) >> shift);
-            atomicAdd(&m.part.count[p], 1u);
-            atomicAdd(&m.part.weight[p], weight_of(s.exponent(x)));
-          }
-        }
-      });
-      __syncthreads();
-      run_up(m.part);
-      const int p = bin_of(m.part, by_count, target - (by_count ? base_c : base_w));
-      const uint32_t c0 = p ? m.part.count[p - 1] : 0;
-      in_bin = m.part.count[p] - c0;
-      base_w += p ? m.part.weight[p - 1] : 0;
-      base_c += c0;
-      const u64 top = hi - ((u64)p << shift), bottom = top - ((1ull << shift) - 1);
-      lo = bottom > lo ? bottom : lo;
-      hi = top;
-      __syncthreads();
-    }
-    each_logit<F32>(row, n, [&](float x, int i) {
-      if (x > -INFINITY && s.bin(x) == b) {
-        const u64 k = make_key(x, i);
-        if (k >= lo && k <= hi) m.sub[atomicAdd(&m.filled, 1u)] = k;
-      }
-    });
+// A row's settings as the caller gave them.
+struct Settings {
+  float T, top_p, min_p, u;
+  int top_k;
+  __device__ __forceinline__ bool good() const {
+    return T >= 0.f && T < INFINITY && top_p >= 0.f && min_p >= 0.f && min_p <= 1.f && u >= 0.f && u < 1.f;
   }
-  __syncthreads();
-  const int filled = (int)m.filled, t = threadIdx.x;
-  const u64 key = t < filled ? m.sub[t] : 0, w = t < filled ? weight_of(s.exponent(key_value(key))) : 0;
-  if (t < filled) m.sub_weight[t] = w;
-  __syncthreads();
-  if (t < filled) {
-    uint32_t c = base_c + 1;
-    u64 sum = base_w + w;
-    for (int j = 0; j < filled; j++) {
-      const bool before = m.sub[j] > key;
-      c += before;
-      sum += before ? m.sub_weight[j] : 0;
-    }
-    if (by_count ? c == target : sum >= target && sum - w < target) m.found_key = key, m.found_weight = sum, m.found_count = c;
-  }
-  __syncthreads();
-  const Place p = {m.found_key, m.found_weight, m.found_count};
-  __syncthreads();
-  return p;
+  __device__ __forceinline__ bool greedy() const { return T == 0.f || top_k == 1; }
+  // the histogram counts only: few enough tokens are picked out, as a rule, to weigh them there
+  __device__ __forceinline__ bool counts_only() const { return top_k > 0 && top_k <= kList / 2; }
+};
+__device__ __forceinline__ Settings settings_of(const SampleCall& c, int64_t r) {
+  return Settings{c.temperatures ? c.temperatures[r] : 1.f, c.top_ps ? c.top_ps[r] : 1.f, c.min_ps ? c.min_ps[r] : 0.f, c.uniforms[r],
+                  c.top_ks ? c.top_ks[r] : 0};
 }
-
+// What the first reading of a row gives: its first token's key (all ones if a logit is NaN or +inf), and the least logit above -inf.
+struct Ends {
+  u64 best;
+  float least;
+  __device__ __forceinline__ bool none() const { return best == ~0ull || key_value(best) == -INFINITY; }
+};
 template <bool F32>
-__global__ void __launch_bounds__(kThreads) k_sample(SampleCall c) {
-  Memory& m = memory();
-  const int64_t r = blockIdx.x;
-  const int t = threadIdx.x;
-  const void* row = (const char*)c.logits + r * c.stride * (F32 ? 4 : 2);
-  const float T = c.temperatures ? c.temperatures[r] : 1.f, top_p = c.top_ps ? c.top_ps[r] : 1.f, min_p = c.min_ps ? c.min_ps[r] : 0.f;
-  const float u = c.uniforms[r];
-  const int top_k = c.top_ks ? c.top_ks[r] : 0;
-  auto answer = [&](int token, double logprob, int kept) {
-    if (t == 0) {
-      c.tokens[r] = token;
-      if (c.logprobs) c.logprobs[r] = (float)logprob;
-      if (c.kept) c.kept[r] = kept;
-    }
-  };
-  if (!(T >= 0.f && T < INFINITY && top_p >= 0.f && min_p >= 0.f && min_p <= 1.f && u >= 0.f && u < 1.f)) return answer(-1, NAN, 0);
-
-  float most = -INFINITY;
+__device__ __forceinline__ Ends ends_of(const void* row, int first, int last) {
+  float most = -INFINITY, least = INFINITY;
+  int at = 0;
   bool bad = false;
-  each_logit<F32>(row, c.vocab, [&](float x, int) {
-    most = fmaxf(most, x);
+  each_logit<F32>(row, first, last, [&](float x, int i) {
+    if (x > most) most = x, at = i;
+    if (x > -INFINITY) least = fminf(least, x);
     bad |= !(x < INFINITY);
   });
-  // the largest in order, a bad row above all
-  const u64 first = group_max(bad ? ~0ull : make_key(most, 0));
-  const float top = key_value(first);
-  if (first == ~0ull || top == -INFINITY) return answer(-1, NAN, 0);
-  if (T == 0.f || top_k == 1) {
-    u64 key = 0;
-    each_logit<F32>(row, c.vocab, [&](float x, int i) {
-      if (x == top) key = max(key, make_key(x, i));
-    });
-    return answer(key_index(group_max(key)), 0.0, 1);
-  }
-
+  // indexes rise within a thread, and a smaller one's key is the larger among equals
+  return Ends{over_group(bad ? ~0ull : make_key(most, at), larger), over_group(least, [](float a, float b) { return fminf(a, b); })};
+}
+__device__ __forceinline__ Scale scale_of(const Settings& z, const Ends& e) {
   Scale s;
-  s.m = top;
-  s.c = 1.4426950408889634 / (double)T;
-  s.bins = (float)fmin(fmax(s.c * ((kBins - 1) / (double)kReach), (double)1.17549435e-38f), (double)3.40282347e+38f);
-  s.most = min_p > 0.f ? -log2((double)min_p) : INFINITY;
-  clear(m.all);
-  if (t == 0) m.bin = 0;
-  __syncthreads();
-  uint32_t likely = 0;  // tokens that min_p keeps
-  each_logit<F32>(row, c.vocab, [&](float x, int) {
-    if (x > -INFINITY) {
-      const double d = s.exponent(x);
-      const u64 w = weight_of(d);
-      const int b = s.bin(x);
-      atomicAdd(&m.all.count[b], 1u);
-      if (w) atomicAdd(&m.all.weight[b], w);
-      likely += d <= s.most;
-    }
-  });
-  __syncthreads();
-  run_up(m.all);
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) likely += (uint32_t)__shfl_xor((int)likely, o, 64);
-  if ((t & 63) == 0) m.wave_a[t >> 6] = likely;
-  __syncthreads();
-  likely = 0;
-  for (int w = 0; w < kWavesOf; w++) likely += (uint32_t)m.wave_a[w];
-  __syncthreads();
+  s.m = key_value(e.best);
+  s.c = 1.4426950408889634 / (double)z.T;
+  // the bins reach to the least logit, or to where weights end
+  const double reach = fmin(((double)s.m - (double)e.least) * s.c, (double)kReach);
+  s.bins = (float)fmin(fmax(s.c * ((kBins - 2) / fmax(reach, 1e-30)), (double)1.17549435e-38f), (double)3.40282347e+38f);
+  s.most = z.min_p > 0.f ? -log2((double)z.min_p) : INFINITY;
+  return s;
+}
+// Adds logits first .. last - 1 to the histogram (cleared, or holding others'). The number of those that min_p keeps, of this thread's.
+template <bool F32>
+__device__ __forceinline__ uint32_t add_up(const void* row, int first, int last, const Scale& s, bool count, bool weigh, bool likely_too) {
+  Memory& m = memory();
+  uint32_t likely = 0;
+  auto all = [&](auto weights) {
+    each_logit<F32>(row, first, last, [&](float x, int) {
+      if (x > -INFINITY) {
+        const int b = s.bin(x);
+        if (count) atomicAdd(&m.all.count[b], 1u);
+        if (decltype(weights)::value || likely_too) {
+          const double d = s.exponent(x);
+          if (decltype(weights)::value) {
+            const u64 w = weight_of(d);
+            if (w) atomicAdd(&m.all.weight[b], w);
+          }
+          likely += d <= s.most;
+        }
+      }
+    });
+  };
+  if (weigh) all(std::true_type{});
+  else all(std::false_type{});
+  return likely;
+}
 
+__device__ __forceinline__ u64 cut_target(float p, u64 weight) { return larger(1, (u64)ceil((double)p * (double)weight)); }
+__device__ __forceinline__ u64 draw_target(float u, u64 weight) {
+  if (weight == 0) return 1;
+  const u64 t = (u64)((double)u * (double)weight);
+  return (t < weight ? t : weight - 1) + 1;
+}
+
+// Bins whose tokens are picked out: up to four stretches.
+struct Wanted {
+  int from[4], to[4];
+  uint32_t tokens;  // at most
+  bool more;        // than stretches 1 and 3
+  __device__ __forceinline__ bool in(int i, int b) const { return (uint32_t)(b - from[i]) <= (uint32_t)(to[i] - from[i]); }
+  // top-k's and the last token's bins are the rarer ones
+  __device__ __forceinline__ bool has(int b) const { return in(1, b) || in(3, b) || (more && (in(0, b) || in(2, b))); }
+};
+// Every bin in which a place of the row can lie, from the running sums: of top-k, of top-p, of the last token that all settings keep, of
+// the draw. With counts alone: all bins up to top-k's.
+__device__ __forceinline__ Wanted wanted_of(const Settings& z, uint32_t likely, bool weighed, int& turn) {
+  const Histogram<kBins>& h = memory().all;
+  Wanted w;
+#pragma unroll
+  for (int i = 0; i < 4; i++) w.from[i] = w.to[i] = kBins;  // none
+  w.tokens = 0;
+  w.more = false;
+  auto count_before = [&](int b) { return b ? h.count[b - 1] : 0u; };
+  auto weight_before = [&](int b) { return b ? h.weight[b - 1] : 0ull; };
+  const uint32_t all = h.count[kBins - 1], k = z.top_k > 0 && (uint32_t)z.top_k < all ? (uint32_t)z.top_k : all;
+  if (!weighed) {
+    w.from[1] = 0;
+    w.to[1] = bin_of(h, true, k, turn);
+    w.tokens = h.count[w.to[1]];
+    return w;
+  }
+  auto add = [&](int i, int a, int b) {
+    w.from[i] = a;
+    w.to[i] = b;
+    w.more |= i % 2 == 0;
+    w.tokens += h.count[b] - count_before(a);
+  };
+  u64 lo = h.weight[kBins - 1], hi = lo;  // bounds of the weight that the draw goes by
+  uint32_t least = k, most = k;           // and of the tokens
+  if (z.top_p < 1.f) {
+    if (k < all) {
+      const int b = bin_of(h, true, k, turn);
+      add(0, b, b);
+      lo = weight_before(b);
+      hi = h.weight[b];
+    }
+    const int a = bin_of(h, false, cut_target(z.top_p, lo), turn), b = bin_of(h, false, cut_target(z.top_p, hi), turn);
+    add(1, a, b);
+    least = count_before(a) + 1;
+    most = h.count[b];
+    lo = weight_before(a);
+    hi = h.weight[b];
+  }
+  if (likely <= most && (likely < all || z.top_p < 1.f || k < all)) {
+    most = likely;
+    const int b = bin_of(h, true, likely, turn);
+    add(2, b, b);
+    lo = likely < least ? weight_before(b) : min(lo, weight_before(b));
+    hi = min(hi, h.weight[b]);
+  } else if (!(z.top_p < 1.f) && k < all) {
+    const int b = bin_of(h, true, k, turn);
+    add(2, b, b);
+    lo = weight_before(b);
+    hi = h.weight[b];
+  }
+  const int a = bin_of(h, false, draw_target(z.u, lo), turn), b = bin_of(h, false, draw_target(z.u, hi), turn);
+  add(3, a, b);
+  return w;
+}
+// Picks the wanted tokens out of logits first .. last - 1: put(key).
+template <bool F32, class Put>
+__device__ __forceinline__ void pick(const void* row, int first, int last, const Scale& s, const Wanted& w, const Put& put) {
+  each_logit<F32>(row, first, last, [&](float x, int i) {
+    if (x > -INFINITY && w.has(s.bin(x))) put(make_key(x, i));
+  });
+}
+
+// Where the count or the weight, in order, reaches `target`, which it does; the row's place number `step`. listed: the list holds the
+// tokens of the wanted bins.
+template <bool F32>
+__device__ __forceinline__ Place find(const void* row, int n, const Scale& s, bool by_count, u64 target, const Wanted& w, bool& listed,
+                                      int& turn, int step) {
+  Memory& m = memory();
+  const int t = threadIdx.x, b = bin_of(m.all, by_count, target, turn);
+  uint32_t base_c = b ? m.all.count[b - 1] : 0, left = m.all.count[b] - base_c;
+  u64 base_w = b ? m.all.weight[b - 1] : 0;
+  u64 lo = 0, hi = ~0ull;  // keys of the bin that are still looked at, `left` of them
+  bool here = listed && w.has(b);
+  auto in_list = [&](auto f) {
+    for (uint32_t i = t; i < m.listed; i += kThreads) {
+      const u64 k = m.list[i];
+      if (k >= lo && k <= hi && s.bin(key_value(k)) == b) f(k);
+    }
+  };
+  auto in_row = [&](auto f) {
+    each_logit<F32>(row, 0, n, [&](float x, int i) {
+      if (x > -INFINITY && s.bin(x) == b) {
+        const u64 k = make_key(x, i);
+        if (k >= lo && k <= hi) f(k);
+      }
+    });
+  };
+  for (;;) {
+    if (!here && left <= kList) {
+      listed = false;  // the list is this bin's now
+      if (t == 0) m.listed = 0;
+      __syncthreads();
+      in_row([&](u64 k) { m.list[atomicAdd(&m.listed, 1u)] = k; });
+      __syncthreads();
+      here = true;
+    }
+    if (here && left <= kFew) break;
+    // divided by the leading bits in which they differ
+    u64 most = 0, least = 0;  // of ~key
+    auto reach = [&](u64 k) {
+      most = larger(k, most);
+      least = larger(~k, least);
+    };
+    if (here) in_list(reach);
+    else in_row(reach);
+    hi = over_group(most, larger);
+    lo = ~over_group(least, larger);
+    const int shift = max(0, 64 - __clzll((long long)(hi - lo)) - 9);
+    clear(m.part);
+    __syncthreads();
+    auto add = [&](u64 k) {
+      const int p = (int)((hi - k) >> shift);
+      atomicAdd(&m.part.count[p], 1u);
+      atomicAdd(&m.part.weight[p], weight_of(s.exponent(key_value(k))));
+    };
+    if (here) in_list(add);
+    else in_row(add);
+    __syncthreads();
+    run_up<true, true>(m.part);
+    const int p = bin_of(m.part, by_count, target - (by_count ? base_c : base_w), turn);
+    const uint32_t c0 = p ? m.part.count[p - 1] : 0;
+    left = m.part.count[p] - c0;
+    base_w += p ? m.part.weight[p - 1] : 0;
+    base_c += c0;
+    const u64 top = hi - ((u64)p << shift), bottom = top - ((1ull << shift) - 1);
+    lo = larger(bottom, lo);
+    hi = top;
+    __syncthreads();
+  }
+  in_list([&](u64 k) { m.few[atomicAdd(&m.filled[step], 1u)] = k; });
+  __syncthreads();
+  const int filled = (int)m.filled[step];
+  if (t < filled) m.few_weight[t] = weight_of(s.exponent(key_value(m.few[t])));
+  __syncthreads();
+  // several threads a token: each looks at every 16th other
+  constexpr int kLanes = kThreads / kFew;
+  const int mine = t / kLanes;
+  const u64 key = mine < filled ? m.few[mine] : 0, weight = mine < filled ? m.few_weight[mine] : 0;
+  uint32_t c = 0;
+  u64 sum = 0;
+#pragma unroll
+  for (int q = 0; q < kFew / kLanes; q++) {
+    const int j = t % kLanes + q * kLanes;
+    const bool before = j < filled && m.few[j] > key;
+    c += before;
+    sum += before ? m.few_weight[j] : 0;
+  }
+#pragma unroll
+  for (int o = kLanes / 2; o >= 1; o >>= 1) {
+    c += (uint32_t)__shfl_xor((int)c, o, 64);
+    sum += __shfl_xor(sum, o, 64);
+  }
+  c += base_c + 1;
+  sum += base_w + weight;
+  if (mine < filled && (by_count ? c == target : sum >= target && sum - weight < target))
+    m.found_key[step] = key, m.found_weight[step] = sum, m.found_count[step] = c;
+  __syncthreads();
+  return Place{m.found_key[step], m.found_weight[step], m.found_count[step]};
+}
+
+// The answer of a row of which the histogram's running sums and, with `listed`, the wanted tokens are at hand.
+template <bool F32>
+__device__ __forceinline__ void draw(const SampleCall& c, int64_t r, const void* row, const Settings& z, const Scale& s, uint32_t likely,
+                                     bool weighed, const Wanted& w, bool listed, int turn) {
+  Memory& m = memory();
+  if (!weighed) {  // the weights of the tokens picked out; where they were too many, of all
+    for (int i = threadIdx.x; i < kBins; i += kThreads) m.all.weight[i] = 0;
+    __syncthreads();
+    if (listed) {
+      for (uint32_t i = threadIdx.x; i < m.listed; i += kThreads) {
+        const float x = key_value(m.list[i]);
+        atomicAdd(&m.all.weight[s.bin(x)], weight_of(s.exponent(x)));
+      }
+    } else {
+      add_up<F32>(row, 0, c.vocab, s, false, true, false);
+    }
+    __syncthreads();
+    run_up<false, true>(m.all);
+  }
   const uint32_t all = m.all.count[kBins - 1];
-  const uint32_t k = top_k > 0 && (uint32_t)top_k < all ? (uint32_t)top_k : all;
-  const bool cut = top_p < 1.f;
-  u64 weight = m.all.weight[kBins - 1];  // of the first `weighed` tokens
-  uint32_t weighed = all, kept = cut ? k : min(k, likely);
+  const uint32_t k = z.top_k > 0 && (uint32_t)z.top_k < all ? (uint32_t)z.top_k : all;
+  const bool cut = z.top_p < 1.f;
+  u64 weight = m.all.weight[kBins - 1];  // of the first `of` tokens
+  uint32_t of = all, kept = cut ? k : min(k, likely);
   Place p;
-  int listed_to = -1;
   // the places asked for, one after the other: top-k's, top-p's, the last one that is kept, the draw
-  for (int step = cut ? 0 : 2; step < 4; step++) {
-    if (step % 2 == 0 && kept == weighed) continue;
-    u64 target = kept;
-    if (step == 1) target = max((u64)1, (u64)ceil((double)top_p * (double)weight));
-    if (step == 3) target = min((u64)((double)u * (double)weight), weight - 1) + 1;
-    p = find<F32>(row, c.vocab, s, step % 2 == 0, target, listed_to);
+#pragma unroll 1
+  for (int step = cut ? 0 : 2; step < kSteps; step++) {
+    if (step % 2 == 0 && kept == of) continue;
+    const u64 target = step == 1 ? cut_target(z.top_p, weight) : step == 3 ? draw_target(z.u, weight) : kept;
+    p = find<F32>(row, c.vocab, s, step % 2 == 0, target, w, listed, turn, step);
     if (step == 3) break;
     weight = p.weight;
-    weighed = p.count;
-    if (step == 1) kept = min(weighed, likely);
+    of = p.count;
+    if (step == 1) kept = min(of, likely);
   }
-  answer(key_index(p.key), -s.exponent(key_value(p.key)) * 0.6931471805599453 - log((double)weight * 0x1p-43), (int)kept);
+  if (threadIdx.x == 0) {
+    c.tokens[r] = key_index(p.key);
+    if (c.logprobs) c.logprobs[r] = (float)(-s.exponent(key_value(p.key)) * 0.6931471805599453 - log((double)weight * 0x1p-43));
+    if (c.kept) c.kept[r] = (int)kept;
+  }
+}
+// The answers that need no draw: true if this is one.
+__device__ __forceinline__ bool answered(const SampleCall& c, int64_t r, const Settings& z, const Ends& e) {
+  const bool none = !z.good() || e.none();
+  if (!none && !z.greedy()) return false;
+  if (threadIdx.x == 0) {
+    c.tokens[r] = none ? -1 : key_index(e.best);
+    if (c.logprobs) c.logprobs[r] = none ? NAN : 0.f;
+    if (c.kept) c.kept[r] = none ? 0 : 1;
+  }
+  return true;
+}
+
+template <bool F32>
+__device__ __forceinline__ const void* row_of(const SampleCall& c, int64_t r) {
+  return (const char*)c.logits + r * c.stride * (F32 ? 4 : 2);
+}
+
+__device__ __forceinline__ void begin() {
+  Memory& m = memory();
+  if (threadIdx.x < kTurns) m.bin[threadIdx.x] = 0;
+  if (threadIdx.x < kSteps) m.filled[threadIdx.x] = 0;
+  if (threadIdx.x == 0) m.listed = 0;
+}
+
+// A row's part of the workspace:
+struct Row {
+  u64 weight[kBins];
+  uint32_t count[kBins];
+  u64 list[kList];
+  uint32_t likely, listed;
+  Wanted wanted;
+};
+struct Layout {
+  size_t rows, ends, bytes;
+};
+__host__ __device__ inline Layout layout_of(int rows, int segments) {
+  Layout l;
+  l.rows = 0;
+  l.ends = (size_t)rows * sizeof(Row);
+  l.bytes = l.ends + (size_t)rows * segments * sizeof(Ends);
+  return l;
+}
+struct Segment {
+  int64_t row;
+  int first, last;
+  Row* state;
+  Ends* ends;  // of the row's segments
+};
+__device__ __forceinline__ Segment segment_of(const SampleCall& c) {
+  Segment g;
+  g.row = blockIdx.y;
+  const int per = ((c.vocab + c.segments - 1) / c.segments + 63) / 64 * 64;  // whole 16 bytes of either type
+  g.first = min((int)blockIdx.x * per, c.vocab);
+  g.last = min(g.first + per, c.vocab);
+  const Layout l = layout_of(c.rows, c.segments);
+  g.state = (Row*)((char*)c.ws + l.rows) + g.row;
+  g.ends = (Ends*)((char*)c.ws + l.ends) + g.row * c.segments;
+  return g;
+}
+__device__ __forceinline__ Ends join_ends(const Segment& g, int segments) {
+  Ends e = {0, INFINITY};
+  for (int i = threadIdx.x & 63; i < segments; i += 64) {  // by each wave for itself, a segment a lane
+    e.best = larger(e.best, g.ends[i].best);
+    e.least = fminf(e.least, g.ends[i].least);
+  }
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) {
+    e.best = larger(e.best, __shfl_xor(e.best, o, 64));
+    e.least = fminf(e.least, __shfl_xor(e.least, o, 64));
+  }
+  return e;
+}
+
+template <bool F32>
+__global__ void __launch_bounds__(kThreads, 8) k_sample_ends(SampleCall c) {
+  const Segment g = segment_of(c);
+  for (int i = blockIdx.x * kThreads + threadIdx.x; i < kBins; i += c.segments * kThreads) g.state->weight[i] = 0, g.state->count[i] = 0;
+  if (blockIdx.x == 0 && threadIdx.x == 0) g.state->likely = g.state->listed = 0;
+  const Ends e = ends_of<F32>(row_of<F32>(c, g.row), g.first, g.last);
+  if (threadIdx.x == 0) g.ends[blockIdx.x] = e;
+}
+template <bool F32>
+__global__ void __launch_bounds__(kThreads, 8) k_sample_add(SampleCall c) {
+  Memory& m = memory();
+  const Segment g = segment_of(c);
+  const Settings z = settings_of(c, g.row);
+  const Ends e = join_ends(g, c.segments);
+  if (!z.good() || e.none() || z.greedy()) return;
+  clear(m.all);
+  __syncthreads();
+  const uint32_t likely = add_up<F32>(row_of<F32>(c, g.row), g.first, g.last, scale_of(z, e), true, !z.counts_only(), z.min_p > 0.f);
+  __syncthreads();
+  for (int i = threadIdx.x; i < kBins; i += kThreads) {
+    if (m.all.count[i]) atomicAdd(&g.state->count[i], m.all.count[i]);
+    if (m.all.weight[i]) atomicAdd(&g.state->weight[i], m.all.weight[i]);
+  }
+  const uint32_t sum = over_group(likely, [](uint32_t a, uint32_t b) { return a + b; });
+  if (threadIdx.x == 0 && sum) atomicAdd(&g.state->likely, sum);
+}
+// The row's running sums in LDS; the tokens that min_p keeps.
+__device__ __forceinline__ uint32_t load_sums(const Segment& g, const Settings& z) {
+  Memory& m = memory();
+  const uint32_t some = g.state->likely;
+  for (int i = threadIdx.x; i < kBins; i += kThreads) m.all.weight[i] = g.state->weight[i], m.all.count[i] = g.state->count[i];
+  begin();
+  __syncthreads();
+  run_up<true, true>(m.all);
+  const uint32_t all = m.all.count[kBins - 1];
+  return z.min_p > 0.f ? some : all;
+}
+template <bool F32>
+__global__ void __launch_bounds__(kThreads, 8) k_sample_pick(SampleCall c) {
+  const Segment g = segment_of(c);
+  const Settings z = settings_of(c, g.row);
+  const Ends e = join_ends(g, c.segments);
+  if (!z.good() || e.none() || z.greedy()) return;
+  int turn = 0;
+  const Wanted w = wanted_of(z, load_sums(g, z), !z.counts_only(), turn);
+  if (blockIdx.x == 0 && threadIdx.x == 0) g.state->wanted = w;
+  if (w.tokens <= kList)
+    pick<F32>(row_of<F32>(c, g.row), g.first, g.last, scale_of(z, e), w, [&](u64 key) { g.state->list[atomicAdd(&g.state->listed, 1u)] = key; });
+}
+template <bool F32>
+__global__ void __launch_bounds__(kThreads) k_sample_draw(SampleCall c) {
+  Memory& m = memory();
+  const Segment g = segment_of(c);
+  const Settings z = settings_of(c, g.row);
+  const Ends e = join_ends(g, c.segments);
+  if (answered(c, g.row, z, e)) return;
+  const Wanted w = g.state->wanted;
+  const bool listed = w.tokens <= kList;
+  const uint32_t likely = load_sums(g, z), n = listed ? min(g.state->listed, (uint32_t)kList) : 0;
+  for (uint32_t i = threadIdx.x; i < n; i += kThreads) m.list[i] = g.state->list[i];
+  if (threadIdx.x == 0) m.listed = n;
+  __syncthreads();
+  draw<F32>(c, g.row, row_of<F32>(c, g.row), z, scale_of(z, e), likely, !z.counts_only(), w, listed, 0);
+}
+
+constexpr int kGroups = 1024;       // workgroups that fill the chip: four a CU
+constexpr int kLeastSegment = 4096;  // logits: with 8192 a single row took 32 us (30), 16 rows 34 to 54 (37 to 58)
+constexpr int kRowsAtOnce = 1024;   // more rows go by several times four launches, which share a workspace
+int segments_of(int rows, int vocab) {
+  return std::max(1, std::min((kGroups + rows - 1) / rows, (vocab + kLeastSegment - 1) / kLeastSegment));
+}
+
+template <class K>
+hipError_t launch(K kernel, dim3 grid, size_t lds, const SampleCall& c, hipStream_t s) {
+  const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+  if (e != hipSuccess) return e;
+  kernel<<<grid, kThreads, lds, s>>>(c);
+  return hipGetLastError();
+}
+template <bool F32>
+hipError_t launch_type(const SampleCall& c, hipStream_t s) {
+  const dim3 grid(c.segments, c.rows);
+  hipError_t e = launch(k_sample_ends<F32>, grid, offsetof(Memory, part), c, s);
+  if (e == hipSuccess) e = launch(k_sample_add<F32>, grid, offsetof(Memory, part), c, s);
+  if (e == hipSuccess) e = launch(k_sample_pick<F32>, grid, offsetof(Memory, part), c, s);
+  if (e == hipSuccess) e = launch(k_sample_draw<F32>, dim3(1, c.rows), sizeof(Memory), c, s);
+  return e;
 }
 
 }  // namespace
 
-size_t sample_ws_bytes(int rows, int vocab) { return 16; }
+size_t sample_ws_bytes(int rows, int vocab) {
+  size_t most = 0;  // the last rows may be cut into more segments
+  for (int r : {std::min(rows, kRowsAtOnce), rows % kRowsAtOnce})
+    if (r > 0) most = std::max(most, layout_of(r, segments_of(r, vocab)).bytes);
+  return most;
+}
 
-hipError_t launch_sample(const SampleCall& c, hipStream_t s) {
-  if (c.rows <= 0) return hipSuccess;
-  const void* kernel = c.f32 ? (const void*)k_sample<true> : (const void*)k_sample<false>;
-  const hipError_t e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Memory));
-  if (e != hipSuccess) return e;
-  if (c.f32) k_sample<true><<<c.rows, kThreads, sizeof(Memory), s>>>(c);
-  else k_sample<false><<<c.rows, kThreads, sizeof(Memory), s>>>(c);
-  return hipGetLastError();
+hipError_t launch_sample(const SampleCall& call, hipStream_t s) {
+  hipError_t e = hipSuccess;
+  for (int r = 0; r < call.rows && e == hipSuccess; r += kRowsAtOnce) {
+    SampleCall c = call;
+    c.rows = std::min(kRowsAtOnce, call.rows - r);
+    c.segments = segments_of(c.rows, c.vocab);
+    c.logits = (const char*)c.logits + r * c.stride * (c.f32 ? 4 : 2);
+    auto skip = [&](auto& p) {
+      if (p) p += r;
+    };
+    skip(c.temperatures);
+    skip(c.top_ks);
+    skip(c.top_ps);
+    skip(c.min_ps);
+    skip(c.uniforms);
+    skip(c.tokens);
+    skip(c.logprobs);
+    skip(c.kept);
+    e = c.f32 ? launch_type<true>(c, s) : launch_type<false>(c, s);
+  }
+  return e;
 }
 
 }  // namespace sidp

@@ -102,6 +102,14 @@ def test_draws_match_the_definition(lib, dtype, rows, vocab):
         check_rows(lib, x, *settings(rng, rows, vocab))
 
 
+@pytest.mark.parametrize("rows", [1024, 1025, 2600])
+def test_more_rows_than_go_at_once(lib, rows):
+    """The last rows, fewer, are cut into more segments than those before them."""
+    rng = np.random.default_rng(rows)
+    x = torch.tensor(rng.standard_normal((rows, 9001)), dtype=torch.float32).to(torch.bfloat16)
+    check_rows(lib, x, *settings(rng, rows, 9001))
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
 @pytest.mark.parametrize("vocab,levels", [(500, 1), (5000, 3), (100000, 1), (100000, 2), (100000, 40)])
 def test_equal_logits_go_by_index(lib, dtype, vocab, levels):
