@@ -646,8 +646,9 @@ int sidp_attention_rows(sidp_handle *h, const void *q, int32_t region, const int
  * and sharing of the work, with a workspace of sidp_attention_rows8_bytes. Codes are
  * multiplied as they are (bf16 holds them), the scale of a key's token with its
  * scores and the scale of a value's token with its weights in fp32, so that the cache's
- * own rounding is the only one beside those of sidp_attention_rows. A row that sees a
- * token without a scale (NaN) is NaN. More rows and heads than one launch covers (2^24
+ * own rounding is the only one beside those of sidp_attention_rows. The weights reach V
+ * with 16 bits in sequences of at most 16 / (Hq / Hkv) rows, rounded to bf16 in longer
+ * ones. A row that sees a token without a scale (NaN) is NaN. More rows and heads than one launch covers (2^24
  * items of 128 / (Hq / Hkv) rows of a sequence and a KV head) are SIDP_EINVAL, and their
  * size is 0. */
 size_t sidp_attention_rows8_bytes(const sidp_handle *h, int32_t batch, int32_t max_rows);
@@ -671,7 +672,8 @@ int sidp_attention_rows8(sidp_handle *h, const void *q, int32_t region, const in
  * half as many tiles of 128 / (Hq / Hkv) rows together as each sequence by itself, or of
  * under 128 shared tokens. The result is that of sidp_attention_rows but for its last
  * bits; the softmax weights of shared tokens reach V with 16 bits in groups of at most
- * 128 / (Hq / Hkv) rows, rounded to bf16 in larger ones.
+ * 128 / (Hq / Hkv) rows (over the 8-bit cache 16 / (Hq / Hkv)), rounded to bf16 in
+ * larger ones.
  * Groups out of order or range, or with a negative length, latch SIDP_EINVAL, as does a
  * shared length past a sequence's own: the rows are right, and nothing is shared (of
  * that group in the second case). A sequence that sidp_attention_rows leaves out is left

@@ -6,7 +6,9 @@
 // of a tile of consecutive rows through LDS, D / 8 lanes a head's token. A block keeps
 // [d / 16][16 tokens][16 dims] of K and [d][16 tokens] of V, so that 16 bytes are a
 // token's 16 dims, or a dim's 16 tokens, and the scales of a block's K and V are one
-// line of 128 bytes. Bound by HBM for prompts, by latency for a token each.
+// line of 128 bytes. Bound by HBM for prompts (about 8200 rows of 64 and 8 heads of 128: 65 us
+// the append, 16 us the reading back, 370 MB together at 4.6 TB/s), by latency for a token
+// each (256 rows with QK-norm 13.5 and 8.5 us, 8 small ones 5 and 4).
 #include "common.h"
 #include "internal.h"
 #include "kv8.h"
