@@ -668,7 +668,7 @@ int sidp_attention_rows8(sidp_handle *h, const void *q, int32_t region, const in
  *                the same blocks for them; the kernels read one sequence's.
  *  groups        0 .. batch; 0: none.
  * Whole chunks of 32 shared tokens are read once, the rest by each sequence as its own;
- * so is everything where it does not pay: a group of which the rows fill no fewer than
+ * so is everything where it does not pay: a group of which the rows fill more than
  * half as many tiles of 128 / (Hq / Hkv) rows together as each sequence by itself, or of
  * under 128 shared tokens. The result is that of sidp_attention_rows but for its last
  * bits; the softmax weights of shared tokens reach V with 16 bits in groups of at most
@@ -733,7 +733,7 @@ int sidp_token_logprobs(const void *logits, int32_t dtype, int32_t rows, int32_t
  * max x) / T). Top-k keeps the first k tokens; top-p, of those, the ones with less than
  * p times the k tokens' weight in front of them, the first one always; min-p the ones
  * with w_i >= min_p. Drawn is the first token, in order, at which the running weight of
- * what all three keep exceeds u times their weight together. Weights are held to 2^-44
+ * what all three keep exceeds u times their weight together. Weights are held to 2^-43
  * of the largest, in whole numbers, so that a row's draw does not depend on the call's
  * other rows nor on the machine. -inf is a masked token (never drawn, never counted). A
  * row without a distribution (a NaN or +inf, or nothing but -inf) or with a setting that

@@ -28,9 +28,9 @@
 // nothing.
 //
 // Measured, us: a row of 128256 bf16 logits 30, 16 rows 37 (top-k and top-p) and 58 (top-p),
-// 64 rows 49 and 78, 256 rows 95 and 137; 256 rows of 151936 fp32 logits with all settings
-// mixed 144, of which the ends take 32 (155 MB at 4.8 TB/s, the only reading from memory);
-// 512 rows of 32001 bf16 logits at a temperature alone 80. What bounds it behind the first
+// 64 rows 50 and 79, 256 rows 95 and 131; 256 rows of 151936 fp32 logits with all settings
+// mixed 137, of which the ends take 32 (155 MB at 4.8 TB/s, the only reading from memory);
+// 512 rows of 32001 bf16 logits at a temperature alone 77. What bounds it behind the first
 // reading is arithmetic on logits, an exponential in 64 bits and two LDS atomics each, and
 // for few rows the barriers of the draw, about 14 us. A workgroup a row for all four steps
 // in one launch took 166 for the mixed rows and 84 for the 512.
@@ -45,8 +45,8 @@ namespace {
 
 typedef unsigned long long u64;
 
-// Waves of a group that goes through barriers together: 8. With 16 the 256 mixed rows took 156 us (144) and a single one 33 (30), with 4
-// they took 174 and 35.
+// Waves of a group that goes through barriers together: 8. With 16 the 256 mixed rows took 156 us and a single one 33, with 8 144 and 30,
+// with 4 174 and 35.
 constexpr int kThreads = 512, kWavesOf = kThreads / 64;
 constexpr int kBins = 2048;
 constexpr float kReach = 44.f;   // weights of 2^-kReach and less are 0
@@ -80,22 +80,28 @@ struct Scale {
   __device__ __forceinline__ int bin(float x) const { return (int)fminf((m - x) * bins, (float)(kBins - 1)); }
 };
 
-// 2^-d in units of 2^-kUnit, to the nearest; d >= 0. The fraction by Taylor's series of exp: the first term left out is
-// (ln 2 / 2)^11 / 11! < 2^-42 of the weight.
+// 2^-d in units of 2^-kUnit, to the nearest; d >= 0. The fraction's power by the polynomial of degree 9 that meets 2^f at the ten
+// Chebyshev nodes of -1/2 .. 1/2: off by at most 2^-45 of it (2 (ln 2 / 4)^10 / 10! = 2^-46 and the coefficients' roundings). Taylor's
+// series would need a degree of 11 for that.
 __device__ __forceinline__ u64 weight_of(double d) {
   if (!(d < kReach + 0.5)) return 0;
-  const double n = __builtin_rint(d), f = (n - d) * 0.6931471805599453;
-  double p = 1.0 / 3628800;
-  p = __builtin_fma(p, f, 1.0 / 362880);
-  p = __builtin_fma(p, f, 1.0 / 40320);
-  p = __builtin_fma(p, f, 1.0 / 5040);
-  p = __builtin_fma(p, f, 1.0 / 720);
-  p = __builtin_fma(p, f, 1.0 / 120);
-  p = __builtin_fma(p, f, 1.0 / 24);
-  p = __builtin_fma(p, f, 1.0 / 6);
-  p = __builtin_fma(p, f, 0.5);
-  p = __builtin_fma(p, f, 1.0);
-  p = __builtin_fma(p, f, 1.0);
+  const double n = __builtin_rint(d), f = n - d;
+  // kept in scalar registers, of which a product takes one operand: in vector ones the ten of them cost the loop 20
+  // (256 mixed rows 149 us, so 137)
+  auto scalar = [](double c) {
+    asm("" : "+s"(c));
+    return c;
+  };
+  double p = 0x1.b6571de2f2351p-24;
+  p = __builtin_fma(p, f, scalar(0x1.63ef969a64d3cp-20));
+  p = __builtin_fma(p, f, scalar(0x1.ffcb76789860fp-17));
+  p = __builtin_fma(p, f, scalar(0x1.43088e257f341p-13));
+  p = __builtin_fma(p, f, scalar(0x1.5d87fe908f88ap-10));
+  p = __builtin_fma(p, f, scalar(0x1.3b2ab72b175eep-7));
+  p = __builtin_fma(p, f, scalar(0x1.c6b08d7044119p-5));
+  p = __builtin_fma(p, f, scalar(0x1.ebfbdff8149f2p-3));
+  p = __builtin_fma(p, f, scalar(0x1.62e42fefa39f7p-1));
+  p = __builtin_fma(p, f, scalar(0x1.000000000003dp+0));
   p = __builtin_amdgcn_ldexp(p, kUnit - (int)n) + 0x1p52;  // the sum's last bit is one unit
   return (u64)__builtin_bit_cast(int64_t, p) & ((1ull << 52) - 1);
 }

@@ -72,6 +72,18 @@ def test_more_tiles_than_the_chip_holds(lib, cache):
     c.close()
 
 
+@pytest.mark.parametrize("groups,prefix", [(2048, 128), (4096, 16)])
+def test_the_most_sequences_and_groups(lib, groups, prefix):
+    """4096 sequences in pairs that share, and each a group of its own."""
+    rng = np.random.default_rng(groups)
+    lens = [(prefix + int(c), int(n)) for c, n in zip(rng.integers(0, 20, 4096), rng.integers(0, 2, 4096))]
+    c = Parts(lib, "bf16", (4, 2, 64), lens, [(4096 // groups, prefix)] * groups, seed=1, regions=1, region=0)
+    out = c.run()
+    close(out[:c.rows], *c.want())
+    assert torch.all(out[c.rows:] == 7.0)
+    c.close()
+
+
 @pytest.mark.parametrize("cache", CACHES)
 def test_the_prefix_is_read_from_one_table(lib, cache):
     """Every other sequence's table is without the prefix's whole chunks: they are the group's, read once."""
