@@ -384,9 +384,24 @@ __device__ __forceinline__ Wanted wanted_of(const Settings& z, uint32_t likely, 
 // Picks the wanted tokens out of logits first .. last - 1: put(key).
 template <bool F32, class Put>
 __device__ __forceinline__ void pick(const void* row, int first, int last, const Scale& s, const Wanted& w, const Put& put) {
-  each_logit<F32>(row, first, last, [&](float x, int i) {
-    if (x > -INFINITY && w.has(s.bin(x))) put(make_key(x, i));
-  });
+  // The stretches as bounds of what Scale::bin cuts to a whole number: up to the last number below `to` + 1, the last bin's end is open.
+  float lo[4], hi[4];
+#pragma unroll
+  for (int i = 0; i < 4; i++) {
+    const bool none = w.from[i] >= kBins;
+    lo[i] = none ? INFINITY : (float)w.from[i];
+    hi[i] = none ? -1.f : w.to[i] == kBins - 1 ? INFINITY : __uint_as_float(__float_as_uint((float)(w.to[i] + 1)) - 1);
+  }
+  auto all = [&](auto more) {  // top-k's and the last token's stretches are the rarer ones
+    each_logit<F32>(row, first, last, [&](float x, int i) {
+      const float at = (s.m - x) * s.bins;
+      bool want = (at >= lo[1] && at <= hi[1]) | (at >= lo[3] && at <= hi[3]);
+      if (decltype(more)::value) want |= (at >= lo[0] && at <= hi[0]) | (at >= lo[2] && at <= hi[2]);
+      if (want && x > -INFINITY) put(make_key(x, i));
+    });
+  };
+  if (w.more) all(std::true_type{});
+  else all(std::false_type{});
 }
 
 // Where the count or the weight, in order, reaches `target`, which it does; the row's place number `step`. listed: the list holds the
