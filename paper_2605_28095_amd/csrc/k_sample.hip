@@ -23,17 +23,16 @@
 // the tokens picked out.
 //
 // Four launches: the row's ends (its largest and least logit), the histogram, the picking,
-// the draw. The first three read the row, from memory the first time, by as many segments
-// as fill the chip; histograms are joined by atomics on whole numbers, whose order changes
-// nothing.
+// the draw. The first three read the row, by as many segments as fill the chip; histograms
+// are joined by atomics on whole numbers, whose order changes nothing.
 //
 // Measured, us: a row of 128256 bf16 logits 30, 16 rows 37 (top-k and top-p) and 58 (top-p),
-// 64 rows 50 and 79, 256 rows 95 and 131; 256 rows of 151936 fp32 logits with all settings
-// mixed 137, of which the ends take 32 (155 MB at 4.8 TB/s, the only reading from memory);
-// 512 rows of 32001 bf16 logits at a temperature alone 77. What bounds it behind the first
-// reading is arithmetic on logits, an exponential in 64 bits and two LDS atomics each, and
-// for few rows the barriers of the draw, about 14 us. A workgroup a row for all four steps
-// in one launch took 166 for the mixed rows and 84 for the 512.
+// 64 rows 49 and 79, 256 rows 92 and 127; 256 rows of 151936 fp32 logits with all settings
+// mixed 135 (146 from Python), of which the ends take 31 (155 MB at 5 TB/s); 512 rows of
+// 32001 bf16 logits at a temperature alone 77. What bounds it is the reading, arithmetic on
+// logits (the histogram 46 us of the mixed rows, with an exponential in 64 bits and two LDS
+// atomics each) and for few rows the barriers of the draw, about 14 us. A workgroup a row
+// for all four steps in one launch took 166 for the mixed rows and 84 for the 512.
 #include <type_traits>
 
 #include "common.h"
