@@ -17,7 +17,7 @@
 // well; with two it is rounded to bf16.
 //
 // bf16 tiles here are of pairs that all see the same keys: a value that is not finite is
-// then nobody's to be kept from.
+// then nobody's to be kept from, and is in both products what it is.
 #pragma once
 #include "attn_tile.h"
 
@@ -33,6 +33,9 @@ constexpr int few_lds() { return kWaves * 16 * NT * (D + 4 + 2) * (int)sizeof(fl
 template <int D, int TYPE, int NT, class Call, class Emit>
 __device__ __forceinline__ void attn_few(const Call& c, const AttnTile<false>& x, int sides, const Emit& emit) {
   constexpr bool kTwo = NT == 1;     // P in two parts
+  // of bf16 the second part gets 2^-23 of the weight more, as in attn_tile.h: a cut that leaves nothing (of a weight of 1, say) would
+  // make 0 * inf of an infinite value. Codes are finite.
+  constexpr float kRest = TYPE ? 1.f : 1.f + 0x1p-23f;
   constexpr int J = D / 64;
   constexpr int kGroupChunks = 32;   // chunks whose block ids a wave holds, two lanes each
   extern __shared__ __attribute__((aligned(16))) char smem[];
@@ -225,7 +228,7 @@ __device__ __forceinline__ void attn_few(const Call& c, const AttnTile<false>& x
         }
         const uint32_t a = __float_as_uint(e[2 * i]), b = __float_as_uint(e[2 * i + 1]);
         hi[i] = __builtin_amdgcn_perm(b, a, 0x07060302u);  // the upper halves
-        lo[i] = pack_bf2(e[2 * i] - __uint_as_float(a & 0xffff0000u), e[2 * i + 1] - __uint_as_float(b & 0xffff0000u));
+        lo[i] = pack_bf2(fmaf(e[2 * i], kRest, -__uint_as_float(a & 0xffff0000u)), fmaf(e[2 * i + 1], kRest, -__uint_as_float(b & 0xffff0000u)));
       }
       p[nt][0] = as_bf16x8(u32x4_t{hi[0], hi[1], hi[2], hi[3]});
       if (kTwo) p[nt][1] = as_bf16x8(u32x4_t{lo[0], lo[1], lo[2], lo[3]});
