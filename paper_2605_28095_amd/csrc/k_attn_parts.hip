@@ -24,26 +24,18 @@
 #include "attn_tile.h"
 #include "common.h"
 #include "internal.h"
+#include "parts_plan.h"
 
 namespace sidp {
 
 namespace {
 
-constexpr int kSlotsPerCu = 2;  // workgroups a CU holds
-// Runs that a tile is cut into: at least this many chunks, at most this many runs, and only where the longest item is this much
-// longer than the runs would be (as in k_attn_rows.hip, which has both sides).
-constexpr int kMinRun = 8, kMaxRuns = 32;
-constexpr float kCutFrom = 1.75f;
-constexpr int kLeastShared = 4;  // chunks
 // Over codes, tiles of up to this many pairs go by attn_few.h, whose waves spread out what they need by themselves (16 sequences of
 // e4m3 over 4000, 5 rows 56 us, 62 by attn_tile.h, 8 rows 61 and 63; 16 rows 96 and 81). Over bf16, 64 pairs over 2048 shared tokens
 // 29 us by it, 26 by attn_tile.h: only 16 pairs go by it.
 constexpr int kFewPairs = 64;
-// Wave items: of at most kWaveShare / 4 of the chunks that a wave has on average, or kWaveLeast.
-constexpr int kWaveShare = 5, kWaveLeast = 4;
 
 __host__ __device__ inline int half_places(int num_cus) { return kSlotsPerCu * (num_cus < 1 ? 1 : num_cus) / 2; }
-__host__ __device__ inline int slots_of(int num_cus, int hkv) { return kSlotsPerCu * (num_cus < 1 ? 1 : num_cus) / hkv; }
 
 enum { kOwnKeys = 1, kOneTile = 2 };  // flags: a row sees the keys up to its own; nobody else reads these keys
 struct Entry {
@@ -61,31 +53,23 @@ struct Cut {
 
 // Workspace: counts, entries, cuts, records (o [row][Hq][D], then m and l [row][Hq][2]).
 struct Layout {
-  int tiles_cap, entries_cap, cuts_cap, recs_cap;  // tiles_cap: of the sequences
+  PartsCaps caps;
   size_t entries, cuts, recs, sums, bytes;
 };
 
 Layout layout_of(int batch, int max_rows, int hq, int hkv, int d, int num_cus, bool groups) {
-  const int tm = tile_tokens(hq / hkv), slots = slots_of(num_cus, hkv);
   Layout l;
-  l.tiles_cap = (int)std::min<int64_t>(max_rows, (int64_t)max_rows / tm + std::min(batch, max_rows));
-  // A group's tiles are at most half of its sequences'. With fewer tiles than slots runs are chosen so that they fit the slots;
-  // with more only shared tiles are cut, into runs of an even share of all chunks or more.
-  l.entries_cap = std::max(l.tiles_cap, slots) + (groups ? l.tiles_cap / 2 + slots : 0);
-  l.cuts_cap = groups ? l.tiles_cap : std::min(l.tiles_cap, std::max(slots, 0));
-  // 2 ceil(R / tm) <= sum ceil(rows / tm) <= R / tm + sequences: R of the groups that share is at most tm a sequence
-  const int64_t shared = groups ? 2 * std::min<int64_t>(max_rows, (int64_t)batch * tm) : 0;
-  l.recs_cap = (int)(shared + (int64_t)slots * std::min(tm, max_rows));
+  l.caps = parts_caps(batch, max_rows, tile_tokens(hq / hkv), slots_of(num_cus, hkv), groups);
   size_t o = 64;
   auto place = [&](size_t n) {
     const size_t at = o;
     o = (o + n + 255) / 256 * 256;
     return at;
   };
-  l.entries = place((size_t)l.entries_cap * sizeof(Entry));
-  l.cuts = place((size_t)l.cuts_cap * sizeof(Cut));
-  l.recs = place((size_t)l.recs_cap * hq * d * sizeof(float));
-  l.sums = place((size_t)l.recs_cap * hq * 2 * sizeof(float));
+  l.entries = place((size_t)l.caps.entries * sizeof(Entry));
+  l.cuts = place((size_t)l.caps.cuts * sizeof(Cut));
+  l.recs = place((size_t)l.caps.recs * hq * d * sizeof(float));
+  l.sums = place((size_t)l.caps.recs * hq * 2 * sizeof(float));
   l.bytes = o;
   return l;
 }
@@ -100,12 +84,11 @@ Layout layout_of(int batch, int max_rows, int hq, int hkv, int d, int num_cus, b
 // as many; 72 under 6 prefixes 51 and 57), and the longest items come first, so that the launch ends evenly. Tiles of few
 // pairs that are short beside a wave's even share are items of a wave each: they are
 // listed apart, behind the others.
-constexpr int kTries = 8;
 constexpr int kPlanWaves = 16;
 __global__ void __launch_bounds__(64 * kPlanWaves) k_attn_parts_plan(AttnPartsCall c, Layout lay) {
   extern __shared__ int32_t s_lds[];
   __shared__ int s_scan[4][kPlanWaves], s_longest[kPlanWaves];
-  __shared__ uint32_t s_total[kPlanWaves];
+  __shared__ ChunkSum s_total[kPlanWaves];
   __shared__ int s_hist[256], s_waves[256], s_listed[2];
   __shared__ int s_items[kTries];
   __shared__ int s_cuts, s_bad;
@@ -182,7 +165,7 @@ __global__ void __launch_bounds__(64 * kPlanWaves) k_attn_parts_plan(AttnPartsCa
     __syncthreads();
     for (int i = t; i < G; i += threads) {
       const int row0 = c.row_starts[s_first[i]], rows = c.row_starts[s_grows[i]] - row0;
-      const bool shares = s_chunks[i] / kChunk >= kLeastShared && s_own[i] > 0 && 2 * ((rows + tm - 1) / tm) <= s_own[i];
+      const bool shares = group_shares(s_chunks[i] / kChunk, rows, s_own[i], tm);
       s_chunks[i] = shares ? s_chunks[i] / kChunk : 0;
       s_grows[i] = shares ? rows : 0;
     }
@@ -229,7 +212,7 @@ __global__ void __launch_bounds__(64 * kPlanWaves) k_attn_parts_plan(AttnPartsCa
     if (t == 0) s_first[G + B] = tiles;
   }
   __syncthreads();
-  tiles = min(tiles, lay.tiles_cap + gtiles);  // row starts that overlap could list more
+  tiles = min(tiles, lay.caps.tiles + gtiles);  // row starts that overlap could list more
   struct Tile {
     int i, place;     // the group, or G and the sequence; which of its tiles
     int rows, from, chunks;
@@ -248,13 +231,12 @@ __global__ void __launch_bounds__(64 * kPlanWaves) k_attn_parts_plan(AttnPartsCa
   auto each_tile = [&](auto f) {
     for (int n = n0; n < n1; n++) f(per == 1 ? only : tile_of(n));
   };
-  uint32_t total = 0;
-  int longest = 1;
+  int own_chunks = 0, longest = 1;
   each_tile([&](const Tile& x) {
-    total += x.chunks;
+    own_chunks += x.chunks;  // at most 2^21 / 1024 tiles of 2^15
     longest = max(longest, x.chunks);
   });
-  const uint32_t own_chunks = total;
+  ChunkSum total = own_chunks;
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) {
     total += __shfl_xor(total, o, 64);
@@ -273,13 +255,13 @@ __global__ void __launch_bounds__(64 * kPlanWaves) k_attn_parts_plan(AttnPartsCa
   const bool few = tiles < slots && tiles <= threads;
   int run = longest;
   if (few) {
-    const int least = max(max((int)(total + slots - 1) / slots, kMinRun), (longest + kMaxRuns - 1) / kMaxRuns);
-    if (longest >= kCutFrom * least) {
-      const int most = max((int)(total + slots - tiles - 1) / (slots - tiles), least);
-      auto try_of = [&](int j) { return least + (most - least) * j / (kTries - 1); };
+    const int least = least_run(total, slots, longest);
+    if (tiles_are_cut(longest, least)) {
+      const int safe = safe_run(total, slots, tiles, least);
+      auto try_of = [&](int j) { return try_run(j, least, safe); };
       int n[kTries];
 #pragma unroll
-      for (int j = 0; j < kTries; j++) n[j] = ((int)own_chunks + try_of(j) - 1) / try_of(j);
+      for (int j = 0; j < kTries; j++) n[j] = (own_chunks + try_of(j) - 1) / try_of(j);
 #pragma unroll
       for (int o = 32; o >= 1; o >>= 1)
 #pragma unroll
@@ -293,12 +275,12 @@ __global__ void __launch_bounds__(64 * kPlanWaves) k_attn_parts_plan(AttnPartsCa
       run = min(run, try_of(j));
     }
   } else if (gtiles > 0 && slots > 0) {
-    run = min(longest, max((int)(total / slots) + 1, kMinRun));
+    run = group_run(total, slots, longest);
   }
   auto parts_of = [&](const Tile& x) { return few || x.i < G ? (x.chunks + run - 1) / run : 1; };
   // places of entries (in order, or by length) and of records
   auto bucket = [&](const Tile& x, int parts) { return 255 - x.chunks / parts * 255 / longest; };
-  const int wave_most = max((int)(total / (kWaves * max(slots, 1))) * kWaveShare / 4, kWaveLeast);
+  const int wave_most = wave_item(total, kWaves, slots, longest);
   auto by_wave = [&](const Tile& x) {
     return !few && x.i >= G && x.rows * group <= 16 && (c.kv8.type != 0 || x.rows == 1) && x.chunks <= wave_most;
   };
@@ -482,7 +464,7 @@ __global__ void __launch_bounds__(256) k_attn_parts_join(AttnPartsCall c, Layout
 
 // Workgroups: as many as there can be items, and one for each round of them, whose wave items are rounded up.
 int64_t grid_of(const Layout& l, int hkv, int num_cus) {
-  const int64_t items = (int64_t)l.entries_cap * hkv;
+  const int64_t items = (int64_t)l.caps.entries * hkv;
   return items + items / half_places(num_cus) + 2;
 }
 
@@ -493,7 +475,7 @@ hipError_t allow_lds(const void* kernel, size_t lds) {
 template <int D, int TYPE>
 hipError_t launch_type(const AttnPartsCall& c, hipStream_t s) {
   const Layout lay = layout_of(c.batch, c.max_rows, c.hq, c.kv.hkv, D, c.num_cus, c.groups > 0);
-  const int waves = std::max(2, std::min(kPlanWaves, (std::max(c.batch, lay.tiles_cap + (c.groups > 0 ? lay.tiles_cap / 2 : 0)) + 63) / 64));
+  const int waves = std::max(2, std::min(kPlanWaves, (std::max(c.batch, lay.caps.tiles + (c.groups > 0 ? lay.caps.tiles / 2 : 0)) + 63) / 64));
   const size_t plan_lds = (4 * (size_t)c.batch + 5 * (size_t)c.groups + 1) * sizeof(int32_t);
   hipError_t e = allow_lds((const void*)k_attn_parts_plan, plan_lds);
   constexpr int lds = std::max(tile_lds<D, TYPE>(), few_lds<D, TYPE ? 2 : 1>());
@@ -503,8 +485,8 @@ hipError_t launch_type(const AttnPartsCall& c, hipStream_t s) {
   k_attn_parts<D, TYPE><<<(unsigned)grid_of(lay, c.kv.hkv, c.num_cus), 256, lds, s>>>(c, lay);
   // workgroups a cut and KV head: as many as its rows need, or as fill the chip
   const int most = (std::min(tile_tokens(c.hq / c.kv.hkv), c.max_rows) * (c.hq / c.kv.hkv) + 1024 / D - 1) / (1024 / D);
-  const int z = std::max<int64_t>(1, std::min<int64_t>(most, 4 * (int64_t)c.num_cus / std::max<int64_t>(1, (int64_t)lay.cuts_cap * c.kv.hkv)));
-  if (lay.cuts_cap > 0) k_attn_parts_join<D><<<dim3(lay.cuts_cap, c.kv.hkv, z), 256, 0, s>>>(c, lay);
+  const int z = std::max<int64_t>(1, std::min<int64_t>(most, 4 * (int64_t)c.num_cus / std::max<int64_t>(1, (int64_t)lay.caps.cuts * c.kv.hkv)));
+  if (lay.caps.cuts > 0) k_attn_parts_join<D><<<dim3(lay.caps.cuts, c.kv.hkv, z), 256, 0, s>>>(c, lay);
   return hipGetLastError();
 }
 template <int D>
