@@ -249,8 +249,8 @@ hipError_t launch_read_d(const Kv8ReadCall& c, hipStream_t s) {
 
 }  // namespace
 
-// HIP's launches have fewer than 2^32 threads.
-bool kv8_read_fits(int rows, int hkv) { return 2 * read_groups(rows, hkv) * 256 < (int64_t)1 << 32; }
+// HIP's launches have fewer than 2^32 threads a dimension: half of them here.
+bool kv8_read_fits(int rows, int hkv) { return read_groups(rows, hkv) * 256 <= (int64_t)1 << 31; }
 
 hipError_t launch_rope_rows8(const RopeRows8Call& c, hipStream_t s) {
   if (c.rows <= 0) return hipSuccess;
