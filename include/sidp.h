@@ -720,7 +720,7 @@ int sidp_token_logprobs(const void *logits, int32_t dtype, int32_t rows, int32_t
  * array that is NULL leaves its setting out.
  *  logits, dtype, rows, vocab, row_stride  as in sidp_token_logprobs; rows at most
  *                SIDP_SAMPLE_MAX_ROWS.
- *  temperatures  device fp32 [rows]: T >= 0; 0 takes the most likely token (NULL: 1).
+ *  temperatures  device fp32 [rows]: T >= 0, finite; 0 takes the most likely token (NULL: 1).
  *  top_ks        device int32 [rows]: k, off at 0 and below and from vocab on.
  *  top_ps        device fp32 [rows]: p >= 0, off from 1 on.
  *  min_ps        device fp32 [rows]: 0 (off) to 1.

@@ -6,9 +6,9 @@
 // Over the 8-bit cache (TYPE other than 0) the same products run on the codes as bf16,
 // which holds them exactly: the scale of a key's token multiplies its scores, with the
 // softmax's own factor, and the scale of a value's token its weights, so that no value
-// is rounded on the way. Chunks come through registers (two of K and of V on their way)
-// and are spread out to bf16 as they are put into LDS, two turns before their scores
-// are made and one before their values are added.
+// is rounded on the way. Chunks come through registers (two of K and one of V on their
+// way) and are spread out to bf16 as they are put into LDS, a turn before their scores
+// are made or their values added.
 #pragma once
 #include <type_traits>
 
@@ -501,22 +501,22 @@ __device__ __forceinline__ void attn_tile(const Call& c, const AttnTile<CAUSAL>&
     const bool carries = kChunkBlocks * D == 64 * kWaves || t < kChunkBlocks * D;
     u32x4_t k_in[2], v_in;
     float s_in;
-    auto load_codes = [&](const uint8_t* cache, int at, int n, bool once, u32x4_t& v) {
+    auto load_codes = [&](const uint8_t* cache, int at, int n, u32x4_t& v) {
       const int place = __builtin_amdgcn_readlane(at, n % kGroupChunks * kChunkBlocks + code_blk);
       if (!carries) return;
-      v = load16<kBlockTokens * D>(cache + (int64_t)place * (kBlockTokens * D), 16 * code_at, once);
+      v = load16<kBlockTokens * D>(cache + (int64_t)place * (kBlockTokens * D), 16 * code_at, false);
     };
-    auto load_k = [&](int n, bool once, u32x4_t& v) {
+    auto load_k = [&](int n, u32x4_t& v) {
       if (n > 0 && n % kGroupChunks == 0) {
         at_k = places(ids_next);
         ids_next = load_ids(c0 + n + kGroupChunks);
       }
-      load_codes(c.kv8.k, at_k, n, once, v);
+      load_codes(c.kv8.k, at_k, n, v);
     };
     int at_s = at_k;
-    auto load_v = [&](int n, bool once, u32x4_t& v) {
+    auto load_v = [&](int n, u32x4_t& v) {
       if (n % kGroupChunks == 0) at_v = at_k;
-      load_codes(c.kv8.v, at_v, n, once, v);
+      load_codes(c.kv8.v, at_v, n, v);
     };
     auto load_s = [&](int n, float& v) {
       if (n % kGroupChunks == 0) at_s = at_k;
@@ -559,12 +559,13 @@ __device__ __forceinline__ void attn_tile(const Call& c, const AttnTile<CAUSAL>&
       // not so small that it is flushed: a masked score stays -inf
       s_scales[slot * (2 * kChunk) + lane] = value ? v : fmaxf(v * scale, 0x1p-126f);
     };
+    // P in one part, and loads that leave what they read in the caches: the fewer pairs that HBM bounds go by attn_few.h.
+    constexpr auto single = std::false_type{};
     // A turn for chunk c0 + n: K(n + 2), V(n) and the scales of n + 1 go to LDS, into the places of K(n), V(n - 2) and the scales of
-    // n - 1, and the registers that held them take K(n + 4), V(n + 2) and the scales of n + 2, these first: they are waited for a turn
-    // before the others. odd: n's last bit. plain: every row sees the chunk whole, and there are those to fetch.
-    auto turn8 = [&](auto first, auto single, auto plain, auto odd, int n, f32x16_t& s, f32x16_t& s_next, bf16x8_t (&p_last)[4],
-                     bf16x8_t (&p)[4]) {
-      constexpr bool kFirst = decltype(first)::value, once = decltype(single)::value, kPlain = decltype(plain)::value;
+    // n - 1, and the registers that held them take K(n + 4), V(n + 1) and the scales of n + 2, these first: all but K's are waited
+    // for a turn later. odd: n's last bit. plain: every row sees the chunk whole, and there are those to fetch.
+    auto turn8 = [&](auto first, auto plain, auto odd, int n, f32x16_t& s, f32x16_t& s_next, bf16x8_t (&p_last)[4], bf16x8_t (&p)[4]) {
+      constexpr bool kFirst = decltype(first)::value, kPlain = decltype(plain)::value;
       constexpr int kOdd = decltype(odd)::value;
       const int ch = c0 + n;
       if (kPlain || n + 2 < n_end) store_k(k_in[kOdd], kOdd);
@@ -573,8 +574,8 @@ __device__ __forceinline__ void attn_tile(const Call& c, const AttnTile<CAUSAL>&
       __builtin_amdgcn_sched_barrier(0);
       if (kPlain || n + 1 < n_end) store_s(s_in, 1 - kOdd, ch + 1);
       if (kPlain || n + 2 < n_end) load_s(n + 2, s_in);
-      if (kPlain || n + 1 < n_end) load_v(n + 1, once, v_in);
-      if (kPlain || n + 4 < n_end) load_k(n + 4, once, k_in[kOdd]);
+      if (kPlain || n + 1 < n_end) load_v(n + 1, v_in);
+      if (kPlain || n + 4 < n_end) load_k(n + 4, k_in[kOdd]);
       if (kPlain ? wave_live : ch * kChunk < wave_most) {
         if (!kPlain) mask(ch, s);
         products(first, single, kOdd, s, s_next, p_last, p);
@@ -583,52 +584,48 @@ __device__ __forceinline__ void attn_tile(const Call& c, const AttnTile<CAUSAL>&
       }
       meet();
     };
-    auto chunks8 = [&](auto single) {
-      constexpr bool once = decltype(single)::value;
-      constexpr auto yes = std::true_type{};
-      constexpr auto no = std::false_type{};
-      constexpr auto even = std::integral_constant<int, 0>{};
-      constexpr auto odd = std::integral_constant<int, 1>{};
-      f32x16_t sa, sb;
-      bf16x8_t pa[4], pb[4];
-      if (t == 64 * (kWaves - 1)) s_odd = 0x7fffffff;  // by the wave that changes it
-      load_s(0, s_in);
-      load_k(0, once, k_in[0]);
-      if (1 < n_end) load_k(1, once, k_in[1]);
-      load_v(0, once, v_in);
-      store_k(k_in[0], 0);
-      store_s(s_in, 0, c0);
-      if (1 < n_end) load_s(1, s_in);
-      if (1 < n_end) store_k(k_in[1], 1);
-      if (2 < n_end) load_k(2, once, k_in[0]);
-      if (3 < n_end) load_k(3, once, k_in[1]);
-      meet();
-      if (c0 * kChunk < wave_most) {
-        const char* kb = smem + k_lane;
+    constexpr auto yes = std::true_type{};
+    constexpr auto no = std::false_type{};
+    constexpr auto even = std::integral_constant<int, 0>{};
+    constexpr auto odd = std::integral_constant<int, 1>{};
+    f32x16_t sa, sb;
+    bf16x8_t pa[4], pb[4];
+    if (t == 64 * (kWaves - 1)) s_odd = 0x7fffffff;  // by the wave that changes it
+    load_s(0, s_in);
+    load_k(0, k_in[0]);
+    if (1 < n_end) load_k(1, k_in[1]);
+    load_v(0, v_in);
+    store_k(k_in[0], 0);
+    store_s(s_in, 0, c0);
+    if (1 < n_end) load_s(1, s_in);
+    if (1 < n_end) store_k(k_in[1], 1);
+    if (2 < n_end) load_k(2, k_in[0]);
+    if (3 < n_end) load_k(3, k_in[1]);
+    meet();
+    if (c0 * kChunk < wave_most) {
+      const char* kb = smem + k_lane;
 #pragma unroll
-        for (int r = 0; r < 16; r++) sa[r] = 0.f;
+      for (int r = 0; r < 16; r++) sa[r] = 0.f;
 #pragma unroll
-        for (int kk = 0; kk < KK; kk++)
-          sa = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(*(const u32x4_t*)(kb + kk * 512)), q[kk], sa, 0, 0, 0);
-      }
-      meet();  // K(0) is read
-      turn8(yes, single, no, even, 0, sa, sb, pb, pa);
-      int n = 1;
-      const int plain_end = min(n_end - 4, (first_pos + 1) / kChunk - c0);
-      for (; n + 1 < plain_end; n += 2) {
-        turn8(no, single, yes, odd, n, sb, sa, pa, pb);
-        turn8(no, single, yes, even, n + 1, sa, sb, pb, pa);
-      }
-      for (; n < n_end; n += 2) {
-        turn8(no, single, no, odd, n, sb, sa, pa, pb);
-        if (n + 1 < n_end) turn8(no, single, no, even, n + 1, sa, sb, pb, pa);
-      }
-      if ((c1 - 1) * kChunk < wave_most) {
-        if (n_end & 1) add_values(single, (n_end - 1) % kRing, pa);
-        else add_values(single, (n_end - 1) % kRing, pb);
-      }
-    };
-    chunks8(std::false_type{});  // of several tiles: for fewer pairs there is attn_few.h
+      for (int kk = 0; kk < KK; kk++)
+        sa = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(*(const u32x4_t*)(kb + kk * 512)), q[kk], sa, 0, 0, 0);
+    }
+    meet();  // K(0) is read
+    turn8(yes, no, even, 0, sa, sb, pb, pa);
+    int n = 1;
+    const int plain_end = min(n_end - 4, (first_pos + 1) / kChunk - c0);
+    for (; n + 1 < plain_end; n += 2) {
+      turn8(no, yes, odd, n, sb, sa, pa, pb);
+      turn8(no, yes, even, n + 1, sa, sb, pb, pa);
+    }
+    for (; n < n_end; n += 2) {
+      turn8(no, no, odd, n, sb, sa, pa, pb);
+      if (n + 1 < n_end) turn8(no, no, even, n + 1, sa, sb, pb, pa);
+    }
+    if ((c1 - 1) * kChunk < wave_most) {
+      if (n_end & 1) add_values(single, (n_end - 1) % kRing, pa);
+      else add_values(single, (n_end - 1) % kRing, pb);
+    }
   } else {
     if (one_tile) chunks(std::true_type{});
     else chunks(std::false_type{});

@@ -475,7 +475,7 @@ __device__ __forceinline__ Place find(const void* row, int n, const Scale& s, bo
   const int filled = (int)m.filled[step];
   if (t < filled) m.few_weight[t] = weight_of(s.exponent(key_value(m.few[t])));
   __syncthreads();
-  // several threads a token: each looks at every 16th other
+  // kLanes threads a token: each looks at every kLanes-th other
   constexpr int kLanes = kThreads / kFew;
   const int mine = t / kLanes;
   const u64 key = mine < filled ? m.few[mine] : 0, weight = mine < filled ? m.few_weight[mine] : 0;
