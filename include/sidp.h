@@ -668,9 +668,12 @@ int sidp_attention_rows8(sidp_handle *h, const void *q, int32_t region, const in
  *                the same blocks for them; the kernels read one sequence's.
  *  groups        0 .. batch; 0: none.
  * Whole chunks of 32 shared tokens are read once, the rest by each sequence as its own;
- * so is everything where it does not pay: a group of which the rows fill more than
- * half as many tiles of 128 / (Hq / Hkv) rows together as each sequence by itself, or of
- * under 128 shared tokens. The result is that of sidp_attention_rows but for its last
+ * so is everything in a group of which the rows fill more than half as many tiles of
+ * 128 / (Hq / Hkv) rows together as each sequence by itself, or of under 128 shared
+ * tokens. What is saved are the bytes that are not read again, at the cost of a join: with
+ * a few sequences, or a few hundred shared tokens, a call without groups may be up to 11
+ * us faster (8 sequences break even past 2048 tokens, 64 at 700 to 1600, 256 at 128 to
+ * 512). The result is that of sidp_attention_rows but for its last
  * bits; the softmax weights of shared tokens reach V with 16 bits in groups of at most
  * 128 / (Hq / Hkv) rows (over the 8-bit cache 16 / (Hq / Hkv)), rounded to bf16 in
  * larger ones.

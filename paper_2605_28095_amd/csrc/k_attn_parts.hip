@@ -12,14 +12,24 @@
 // instead of n, and its products fill the matrices' columns, G being Hq / Hkv.
 //
 // Only whole chunks of 32 tokens are shared; the rest of the prefix is read by each
-// sequence as its own. A group shares where its tiles are at most half of its sequences'.
+// sequence as its own. A group shares where its tiles are at most half of its sequences'
+// (parts_plan.h, where the rules of the plan stand with what both their sides measured).
+//
+// P reaches V with 16 bits in tiles of attn_few.h with up to 16 pairs, and over bf16 in all
+// tiles of a sequence or group of one tile; rounded to bf16 in the others. Rounded and in two
+// parts there, us a call: 256 rows under 8192 shared bf16 tokens 137 and 162, 64 under 4096 43
+// and 47; 8 ragged chunks of e4m3 280 and 367, of int8 299 and 388; 16 sequences of 1-7 rows over
+// int8 46 and 48, of 8 rows over 4000 59 and 64. Distance from 64 bits 0.0021 to 0.0023 of the norm,
+// 0.0017 with 16 bits, which is what the result's own rounding makes.
 //
 // Measured with 64 and 8 heads of 128, us with plan and join: over e4m3 64 sequences of a row
-// with 1-8K keys 119 (625 MB, 5.6 TB/s in the kernel itself), 8 ragged chunks 373-390 (323
-// GFLOP, matrix units 40% and vector issue 47%, held by what each waits for of the other);
-// over int8 16 sequences of 1-7 rows with 0.5-4K keys 41; 256 sequences of a row over 8192
-// shared keys of bf16 135-142 (566 MB, 8.6 GB if each read them itself); 72 over 6
-// prefixes of e4m3 50, of which plan and join are 17: one workgroup in front of all.
+// with 1-8K keys 119-131 (625 MB, 5.6 TB/s in the kernel itself), over int8 134-143; 8 ragged
+// chunks of 234 to 348 GFLOP, as lengths meet, 280-410 over e4m3 (0.80 to 0.87 PFLOP/s: matrix
+// units 40% and vector issue 47%, held by what each waits for of the other), 300-440 over int8;
+// 16 sequences of 1-7 rows with 0.5-4K keys 41-46 over int8, 41 over e4m3; 256 sequences of a
+// row over 8192 shared keys of bf16 135-147 (566 MB, 8.6 GB if each read them itself), of
+// e4m3 146-151, of int8 161; 72 over 6 prefixes of e4m3 50, of int8 51, of which plan and join
+// are 17: one workgroup in front of all.
 #include "attn_few.h"
 #include "attn_tile.h"
 #include "common.h"
@@ -30,9 +40,11 @@ namespace sidp {
 
 namespace {
 
-// Over codes, tiles of up to this many pairs go by attn_few.h, whose waves spread out what they need by themselves (16 sequences of
-// e4m3 over 4000, 5 rows 56 us, 62 by attn_tile.h, 8 rows 61 and 63; 16 rows 96 and 81). Over bf16, 64 pairs over 2048 shared tokens
-// 29 us by it, 26 by attn_tile.h: only 16 pairs go by it.
+// Over codes, tiles of up to this many pairs go by attn_few.h, whose waves spread out what they need by themselves. By it and by
+// attn_tile.h, us a call, 16 sequences over 4000 keys, heads of 128: 24 pairs e4m3 41 and 45, int8 43 and 48; 40 pairs 49 and 53, 57
+// and 55; 64 pairs 52 and 54, 60 and 57. Heads of 64: 24 pairs 32 and 39, 33 and 42; 64 pairs 41 and 46, 44 and 49. Over 500 keys the
+// two are within 2 us. 128 pairs of e4m3 96 and 81. Over bf16, 64 pairs over 2048 shared tokens 29 us by it, 26 by attn_tile.h: only
+// 16 pairs go by it.
 constexpr int kFewPairs = 64;
 
 __host__ __device__ inline int half_places(int num_cus) { return kSlotsPerCu * (num_cus < 1 ? 1 : num_cus) / 2; }

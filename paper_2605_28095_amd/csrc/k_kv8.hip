@@ -7,8 +7,11 @@
 // [d / 16][16 tokens][16 dims] of K and [d][16 tokens] of V, so that 16 bytes are a
 // token's 16 dims, or a dim's 16 tokens, and the scales of a block's K and V are one
 // line of 128 bytes. Bound by HBM for prompts (about 8200 rows of 64 and 8 heads of 128: 65 us
-// the append, 16 us the reading back, 370 MB together at 4.6 TB/s), by latency for a token
-// each (256 rows with QK-norm 13.5 and 8.5 us, 8 small ones 5 and 4).
+// the append, 319 MB at 4.9 TB/s, 16 us the reading back, 51 MB at 3.1), by latency for a token each
+// (256 rows with QK-norm 13.5 and 8.5 us, 8 small ones 5 and 4). The bf16 append of 256 rows takes
+// 8: here a token by itself goes through the largest of its dims and the list of pieces
+// as a prompt's do; which of them makes the difference was not measured. int8 takes the same times, its
+// divisions included.
 #include "common.h"
 #include "internal.h"
 #include "kv8.h"

@@ -7,13 +7,25 @@
 namespace sidp {
 
 constexpr int kSlotsPerCu = 2;  // workgroups a CU holds
-// Runs that a tile is cut into: at least this many chunks, at most this many runs, and only where the longest item is this much
-// longer than the runs would be (as in k_attn_rows.hip, which has both sides).
+// Runs that a tile is cut into: at least kMinRun chunks, at most kMaxRuns runs, and only where the longest item is kCutFrom times as
+// long as the runs would be (k_attn_rows.hip has both sides of the latter two). Runs of at least 8 chunks, of 16 and of 4, us a call:
+// 4 sequences under 1024 shared bf16 tokens 25, 29, 24; 8 under 2048 28, 31, 28; 32 under 1024 28, 30, 29; over e4m3 1 row of 1000
+// 18, 20, 18; 4 x 40 rows of 2000 46, 48, 45; but 16 x 1 of 500 20, 18, 20 and 4 x 1 of 4000 25, 23, 25; longer ones alike.
 constexpr int kMinRun = 8, kMaxRuns = 32;
 constexpr float kCutFrom = 1.75f;
 constexpr int kTries = 8;
-constexpr int kLeastShared = 4;  // chunks
-// Wave items: of at most kWaveShare / 4 of the chunks that a wave has on average, or kWaveLeast.
+// Chunks of the shortest prefix that is shared. What sharing costs is the join and the group's items (1 to 11 us); what it saves are
+// the bytes of the prefix for all rows but one tile's, so that 128 tokens are about where it begins to pay, in calls with many KV
+// heads and rows, and few sequences want far more. Shared and not, us a call: 256 rows in 8 groups, 16 heads of 64, bf16, under 128
+// 66.5 and 67.5, 192 67 and 73, 256 67 and 77; 256 rows in 32 groups, 8 KV heads of 128, bf16, under 128 75 and 76, 192 78 and 87,
+// 1024 95 and 193; the same over e4m3 under 128 57 and 50, 256 60 and 63, 1024 61 and 107; 64 rows in 8, bf16, under 256 34 and 28,
+// 768 35 and 37, 2048 45 and 65; 8 rows in 1 under 256 27 and 21, 2048 28 and 25.
+constexpr int kLeastShared = 4;
+// Wave items: of at most kWaveShare / 4 of the chunks that a wave has on average, or kWaveLeast. With them and without, us a call,
+// rows of one with so many keys each: e4m3 512 of 0-300 53 and 63, 256 of 200 34 and 41, 256 of 0-1000 69 and 68; 256 under 8192
+// shared bf16 tokens 143 and 150; but where a sequence is about a wave's share and items are few, a launch waits for the waves that
+// start last: e4m3 128 of 500-1500 68 and 58, 128 of 0-8000 195 and 181. At 3 / 4 of the average 58 and 183 there, 57, 41 and 70 in
+// the first ones; at 10 / 4 69 and 258, and 53, 34 and 73.
 constexpr int kWaveShare = 5, kWaveLeast = 4;
 
 // Chunks of all tiles: a million rows of 4 a tile are 2^18 tiles, of up to 2^15 chunks each.
@@ -26,7 +38,10 @@ constexpr int at_most(ChunkSum n, int most) { return n < (ChunkSum)most ? (int)n
 // For one KV head's items.
 constexpr int slots_of(int num_cus, int hkv) { return kSlotsPerCu * larger_of(num_cus, 1) / hkv; }
 
-// A group shares its prefix where its tiles are at most half of its sequences'.
+// A group shares its prefix where its tiles are at most half of its sequences'. Shared all the same, which halves nothing but leaves
+// records of every row, 32 sequences of 9 rows (18 tiles, not 32) take 41, 52 and 96 us under 256, 1024 and 4096 bf16 tokens and 43,
+// 62 and 134 over e4m3; not shared 27, 59, 110 and 25, 54, 99. 16 sequences 30, 40, 53 and 32, 43, 61; not shared 26, 43, 68 and 24,
+// 40, 62.
 constexpr bool group_shares(int shared_chunks, int group_rows, int own_tiles, int tm) {
   return shared_chunks >= kLeastShared && own_tiles > 0 && 2 * ((group_rows + tm - 1) / tm) <= own_tiles;
 }
