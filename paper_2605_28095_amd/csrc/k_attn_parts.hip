@@ -245,7 +245,7 @@ __global__ void __launch_bounds__(64 * kPlanWaves) k_attn_parts_plan(AttnPartsCa
   };
   int own_chunks = 0, longest = 1;
   each_tile([&](const Tile& x) {
-    own_chunks += x.chunks;  // at most 2^21 / 1024 tiles of 2^15
+    own_chunks += x.chunks;  // at most 2^18 / 1024 tiles of 2^15
     longest = max(longest, x.chunks);
   });
   ChunkSum total = own_chunks;

@@ -28,7 +28,7 @@ constexpr int kLeastShared = 4;
 // the first ones; at 10 / 4 69 and 258, and 53, 34 and 73.
 constexpr int kWaveShare = 5, kWaveLeast = 4;
 
-// Chunks of all tiles: a million rows of 4 a tile are 2^18 tiles, of up to 2^15 chunks each.
+// Chunks of all tiles: a million rows of 8 a tile are more than 2^17 tiles, of up to 2^15 chunks each.
 typedef uint64_t ChunkSum;
 
 constexpr int larger_of(int a, int b) { return a > b ? a : b; }

@@ -116,26 +116,28 @@ def chunks_of(rows, ctx, tm):
 
 
 def longest_call():
-    """2048 sequences of a row in groups of four under 2^14 chunks, and as many of 508 rows whose 260096 tiles' chunks sum to just more
-    than 2^32."""
-    tm, n, rows, prefix = 4, 2048, 508, 1 << 14
-    rest = 512 * prefix + n  # the groups' tiles, and what is left of their sequences
-    ctx = next(c for c in range(32 * 16384, 32 * 16640) if n * chunks_of(rows, c, tm) + rest >= 1 << 32)
-    assert n * chunks_of(rows, ctx, tm) + rest < (1 << 32) + (1 << 18)
-    groups = [(4 * i, 4 * i + 4, prefix) for i in range(n // 4)]
-    return n + rows * n, tm, 512, [(1, 32 * prefix)] * n + [(rows, ctx)] * n, groups
+    """16 query heads of one KV head, tiles of 8 rows: 72 sequences of a row in groups of eight under 32000 chunks, and 4024 of 257 rows,
+    whose 132792 tiles' chunks sum to just more than 2^32."""
+    tm, n, rows, prefix = 8, 4024, 257, 32000
+    rest = 9 * prefix + 72  # the groups' tiles, and what is left of their sequences
+    ctx = next(c for c in range(32 * 32000, (1 << 20) - rows, 8) if n * chunks_of(rows, c + 8, tm) + rest >= 1 << 32)
+    short, each = (1 << 32) - rest - n * chunks_of(rows, ctx, tm), chunks_of(rows, ctx + 8, tm) - chunks_of(rows, ctx, tm)
+    longer = -(-short // each)  # so many of them have 8 keys more
+    assert 0 < longer <= n and each < 32
+    groups = [(8 * i, 8 * i + 8, prefix) for i in range(9)]
+    return 72 + rows * n, tm, 512, [(1, 32 * prefix)] * 72 + [(rows, ctx + 8)] * longer + [(rows, ctx)] * (n - longer), groups
 
 
 def test_the_longest_lists_fit(plan):
     """A million rows over the longest caches; groups' runs are of an even share of it all."""
     call = longest_call()
-    assert call[0] <= 1 << 20
+    assert call[0] <= 1 << 20 and len(call[3]) <= 4096
     (found,) = lists(plan, [call])
     assert fits(found), found
-    assert found[0] == 512 + 2048 * 127 + 2048  # an even share of all is longer than any tile: nothing is cut
-    full = [(1 << 20, 1, 512, [(256, (1 << 20) - 256)] * 4096, []), (1 << 20, 4, 1, [(256, (1 << 20) - 256)] * 4096, []),
+    assert found[0] == 9 + 4024 * 33 + 72  # an even share of all is longer than any tile: nothing is cut
+    full = [(1 << 20, 8, 512, [(256, (1 << 20) - 256)] * 4096, []), (1 << 20, 8, 1, [(256, (1 << 20) - 256)] * 4096, []),
             (1 << 20, 128, 0, [(256, (1 << 20) - 256)] * 4096, [(0, 4096, 32760)]),
-            (4096, 128, 64, [(1, (1 << 20) - 1)] * 4096, [(0, 4096, 32767)]), (4096, 1, 1, [(1, (1 << 20) - 1)] * 4096, [(0, 4096, 32767)])]
+            (4096, 128, 64, [(1, (1 << 20) - 1)] * 4096, [(0, 4096, 32767)]), (4096, 8, 1, [(1, (1 << 20) - 1)] * 4096, [(0, 4096, 32767)])]
     for found in lists(plan, full):
         assert fits(found), found
 
@@ -155,7 +157,7 @@ def test_lists_of_all_kinds_fit(plan):
     calls = []
     for _ in range(400):
         B = int(np.exp(rng.uniform(0, np.log(4096))))
-        tm = int(rng.choice([1, 2, 4, 8, 16, 25, 32, 64, 128]))
+        tm = 128 // int(rng.integers(1, 17))
         slots = int(rng.choice([0, 1, 2, 7, 32, 64, 128, 256, 512]))
         most_rows = max(1, min(int(np.exp(rng.uniform(0, np.log(400)))), (1 << 20) // B))
         rows = rng.integers(0, most_rows + 1, B) if rng.random() < 0.7 else rng.integers(0, 2, B)
