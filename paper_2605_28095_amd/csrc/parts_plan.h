@@ -8,9 +8,11 @@ namespace sidp {
 
 constexpr int kSlotsPerCu = 2;  // workgroups a CU holds
 // Runs that a tile is cut into: at least kMinRun chunks, at most kMaxRuns runs, and only where the longest item is kCutFrom times as
-// long as the runs would be (k_attn_rows.hip has both sides of the latter two). Runs of at least 8 chunks, of 16 and of 4, us a call:
+// long as the runs would be (k_attn_rows.hip has both sides of that). Runs of at least 8 chunks, of 16 and of 4, us a call:
 // 4 sequences under 1024 shared bf16 tokens 25, 29, 24; 8 under 2048 28, 31, 28; 32 under 1024 28, 30, 29; over e4m3 1 row of 1000
-// 18, 20, 18; 4 x 40 rows of 2000 46, 48, 45; but 16 x 1 of 500 20, 18, 20 and 4 x 1 of 4000 25, 23, 25; longer ones alike.
+// 18, 20, 18; 4 x 40 rows of 2000 46, 48, 45; but 16 x 1 of 500 20, 18, 20 and 4 x 1 of 4000 25, 23, 25; longer ones alike. At most
+// 32 runs, 16 and 64: over e4m3 1 row of 32000 34, 37, 41, 5 rows 45, 57, 49; 8 rows under 32000 shared bf16 tokens 52, 62, 62; but 1
+// row of 8000 26, 24, 25.
 constexpr int kMinRun = 8, kMaxRuns = 32;
 constexpr float kCutFrom = 1.75f;
 constexpr int kTries = 8;
@@ -23,9 +25,8 @@ constexpr int kTries = 8;
 constexpr int kLeastShared = 4;
 // Wave items: of at most kWaveShare / 4 of the chunks that a wave has on average, or kWaveLeast. With them and without, us a call,
 // rows of one with so many keys each: e4m3 512 of 0-300 53 and 63, 256 of 200 34 and 41, 256 of 0-1000 69 and 68; 256 under 8192
-// shared bf16 tokens 143 and 150; but where a sequence is about a wave's share and items are few, a launch waits for the waves that
-// start last: e4m3 128 of 500-1500 68 and 58, 128 of 0-8000 195 and 181. At 3 / 4 of the average 58 and 183 there, 57, 41 and 70 in
-// the first ones; at 10 / 4 69 and 258, and 53, 34 and 73.
+// shared bf16 tokens 143 and 150; but with few items, some of them about as long as a wave's share, e4m3 128 of 500-1500 68 and 58,
+// 128 of 0-8000 195 and 181. With 3 / 4 of the average 57, 41 and 70, 58 and 183; with 10 / 4 53, 34 and 73, 69 and 258.
 constexpr int kWaveShare = 5, kWaveLeast = 4;
 
 // Chunks of all tiles: a million rows of 8 a tile are more than 2^17 tiles, of up to 2^15 chunks each.
